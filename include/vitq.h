@@ -364,6 +364,160 @@ vq_status vq_vit_encoder_workspace(const vq_preln_desc *layers, int32_t n_layers
 vq_status vq_vit_encoder(const vq_preln_desc *layers, int32_t n_layers, const float *x, int64_t B,
                          float *y_out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Operators of a language model's serving layer -----------------------------------------------
+ * The floating-point siblings of the entry points above, for the layers that serve text next to an
+ * integerized image tower: 8-bit floats with a scale per block of 128 in place of integer levels,
+ * queries and keys normalised per head and rotated by their position, keys and values kept in a
+ * paged cache, and attention of new tokens over it.  In the order of their use:
+ *     vq_quantize_e4m3 -> vq_linear_e4m3 (Q, K, V) -> vq_qkv_norm_rotate -> vq_attention_paged
+ *     -> vq_quantize_e4m3 -> vq_linear_e4m3 (output)
+ * The conventions at the top of this file hold: nothing is allocated, read back or synchronized, so
+ * every call may be captured into a graph and replayed.  A workspace or an output must not be shared
+ * by calls that overlap in time.  Inference only: there are no gradients.
+ */
+typedef enum vq_dtype {
+    VQ_F32 = 0,
+    VQ_BF16 = 1,
+    VQ_F16 = 2,
+    VQ_E4M3 = 3 /* 1 sign, 4 exponent, 3 mantissa bits, bias 7, largest 448, no infinities */
+} vq_dtype;
+
+/*
+ * A matrix of E4M3 values in device memory with one fp32 scale per block of 128 columns and
+ * block_rows (1 or 128) rows: value (r, c) = code(r, c) * scales[(c/128)*scale_stride + r/block_rows].
+ * Code (r, c) is the byte r*row_stride + c.  row_stride (bytes) is a multiple of 16 and data 16-byte
+ * aligned; in an INPUT the bytes from cols up to the next multiple of 16 must be zero, in an OUTPUT
+ * the library writes them (zero) and nothing beyond.  scale_stride (elements) >= ceil(rows/block_rows).
+ */
+typedef struct vq_fmat {
+    void *data;
+    float *scales;
+    int32_t block_rows;
+    int32_t reserved;
+    int64_t rows, cols;
+    int64_t row_stride;
+    int64_t scale_stride;
+} vq_fmat;
+
+/*
+ * Quantizer to that format.  Per block: a = max(max |x|, 2^-100); scale = a / 448; code = x * (448 / a)
+ * rounded to the nearest E4M3 value, ties to even (every operation a correctly rounded fp32 one).
+ * A NaN anywhere in a block makes its scale and all its codes NaN; an infinity makes the scale infinite.
+ * x: device, x_dtype VQ_F32, VQ_BF16 or VQ_F16, [rows x cols], leading dimension ld (elements), at any
+ * alignment of its type (16-byte aligned rows are read faster).  Limits: rows <= 2^27, cols <= 2^22.
+ * Errors: NULL, SHAPE, BITS (x_dtype), STRIDE, UNSUPPORTED (block_rows neither 1 nor 128).
+ */
+vq_status vq_quantize_e4m3(const void *x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ld,
+                           const vq_fmat *out, void *stream);
+
+/*
+ * y[m][n] = act(sum_j xs[j][m] * ws[j][n/128] * (sum over k in block j of x[m][k] * w[n][k]) + bias[n])
+ * rounded once to y_dtype (VQ_F32, VQ_BF16 or VQ_F16); sums over blocks, bias and activation in fp32.  Inside a block,
+ * VQ_F32 results have exact products and fp32 sums.  The 16-bit results come from the 8-bit matrix cores at twice the rate:
+ * of each sixteen products (columns 16i .. 16i+15) what lies more than 2^13 below the largest is dropped, which is a
+ * tenth of a half-precision result's own rounding for normal data.
+ * x: [M x K], block_rows 1; w: [Nout x K], block_rows 128 (else UNSUPPORTED).  bias: device fp32
+ * [Nout] or NULL.  act: 0 none, 1 GELU (tanh form).  y: device [M x Nout], leading dimension ld
+ * (elements), aligned to its type.  Limits: K <= 65536, row strides of both operands below 2^24 bytes.
+ * The order of the sums depends on the sizes alone: equal calls give equal bits.
+ * Errors: NULL, SHAPE, BITS (y_dtype), STRIDE, UNSUPPORTED.
+ */
+vq_status vq_linear_e4m3(const vq_fmat *x, const vq_fmat *w, const float *bias, int32_t act, void *y,
+                         int32_t y_dtype, int64_t ld, void *stream);
+
+/*
+ * A paged cache of keys and values: `pages` pages of `page_size` tokens (any size).  Element
+ * (page, head, place in the page, channel) is at page*page_stride + head*head_stride +
+ * place*token_stride + channel (elements; the same strides for k and v), so pages may hold heads or
+ * tokens first.  dtype: VQ_BF16, VQ_F16 or VQ_E4M3 (then a key is code * k_scale, a value code *
+ * v_scale; else both scales must be 1).  Strides are multiples of 16 bytes, k and v 16-byte aligned,
+ * all of k (v) lies within 2^36 bytes, and pages * page_size < 2^31.  Slot numbers count tokens: slot = page*page_size + place.
+ */
+typedef struct vq_kv_cache {
+    void *k, *v;
+    int32_t dtype, heads, head_dim, page_size;
+    int64_t pages;
+    int64_t page_stride, head_stride, token_stride;
+    float k_scale, v_scale;
+} vq_kv_cache;
+
+/*
+ * Per-head norm of queries and keys, rotation by position, and the keys' and values' way into the
+ * cache, in one pass over the output of a fused Q, K, V projection.  Token t's row of qkv holds q_heads
+ * queries, kv_heads keys and kv_heads values of head_dim channels each.  For a query or key head v:
+ *     norm 1 (RMS):       v = v / sqrt(mean(v^2) + eps) * gamma
+ *     norm 2 (LayerNorm): v = (v - mean v) / sqrt(var v + eps) * gamma + beta
+ *     norm 0:             v as it is
+ * then the first rot_dim channels turn in pairs (a, b) -> (a*c - b*s, b*c + a*s) by the angles of row
+ * positions[t] of the tables (c = cos, s = sin, fp32 [table_rows x rot_dim/2]): pair i is the channels
+ * (i, i + rot_dim/2), or (2i, 2i+1) if interleaved.  Any rotation is one of its tables: two-dimensional
+ * positions of image tokens are a table with one row per place.  All in fp32, rounded once.
+ * gamma / beta: device fp32 [head_dim] for all heads (gamma_head_stride 0) or one row per head
+ * (gamma_head_stride >= head_dim, elements, a multiple of 4); beta nullable.  gamma, beta and the
+ * tables are 16-byte aligned.
+ */
+typedef struct vq_rotate_desc {
+    int32_t q_heads, kv_heads, head_dim;
+    int32_t norm;         /* 0 none, 1 RMS, 2 LayerNorm                                         */
+    int32_t rot_dim;      /* 0: no rotation; else a multiple of 16 up to head_dim                */
+    int32_t interleaved;
+    const float *q_gamma, *q_beta, *k_gamma, *k_beta;
+    int64_t gamma_head_stride;
+    const float *cos_table, *sin_table;
+    int64_t table_rows;
+    float eps;
+    int32_t reserved;
+} vq_rotate_desc;
+
+/*
+ * qkv: device, dtype VQ_F32, VQ_BF16 or VQ_F16, [tokens x (q_heads + 2*kv_heads)*head_dim], leading
+ * dimension ld.  positions: device int32 [tokens]; NULL only if rot_dim is 0.  q_out: device, q_dtype
+ * VQ_BF16 or VQ_F16, [tokens x q_heads*head_dim], leading dimension q_ld; NULL: queries are not wanted.
+ * cache, slots (device int64 [tokens]): where each token's key and value go; both NULL: keys and values
+ * are not wanted.  For E4M3 a value is multiplied by the fp32 reciprocal of the scale, limited to
+ * +-448 and rounded (NaN stays NaN).  qkv and q_out: 16-byte aligned, with ld and q_ld multiples of 16
+ * bytes; qkv must not overlap the outputs.  A token whose position lies outside the table is padding:
+ * nothing of it is written.  A slot outside [0, pages*page_size) (-1, say) is not written.  The slots
+ * that are written must differ from each other.  head_dim: a multiple of 8 up to 256 (E4M3: of 16);
+ * tokens <= 2^23.
+ * Errors: NULL, SHAPE, BITS (a dtype), STRIDE, STEP (eps, a scale), UNSUPPORTED.
+ */
+vq_status vq_qkv_norm_rotate(const vq_rotate_desc *desc, const void *qkv, int32_t dtype, int64_t tokens,
+                             int64_t ld, const int32_t *positions, void *q_out, int32_t q_dtype,
+                             int64_t q_ld, const vq_kv_cache *cache, const int64_t *slots, void *stream);
+
+/*
+ * Attention of new tokens over the cache, for ragged batches of sequences from single tokens to whole
+ * prompts.  Sequence s has the query rows q_offsets[s] .. q_offsets[s+1]-1 and the keys 0 ..
+ * kv_lens[s]-1, the new tokens' own among them (they are the last); key j is token j % page_size of page
+ * page_table[s*table_stride + j / page_size].  Row i of the n new tokens stands at place p = kv_lens[s]
+ * - n + i and sees key j if j < kv_lens[s], (causal) j <= p, and (window > 0) j > p - window.  Query
+ * head h reads key-value head h / (q_heads / cache->heads).
+ *     out = sum_j softmax_j(scale * q . k_j) * v_j;   lse = log(sum_j exp(scale * q . k_j))
+ * A row that sees no key gets out 0 and lse -infinity.  Keys on a page number outside [0, pages) are
+ * not seen, and rows outside every sequence are left as they were.
+ * q, out: device, dtype VQ_BF16 or VQ_F16, [tokens x q_heads*head_dim], leading dimensions q_ld, out_ld,
+ * 16-byte aligned with strides of multiples of 16 bytes; out may be q itself.  q_offsets: device int32
+ * [seqs + 1], not decreasing.  kv_lens: device int32 [seqs].  page_table: device int32 [seqs x
+ * table_stride], of which the first table_cols of a row are page numbers; kv_lens beyond
+ * table_cols*page_size are cut there.  lse: device fp32 [tokens x q_heads] or NULL.
+ * max_kv: the longest kv_len that the caller expects (0: table_cols*page_size); it steers how the keys
+ * are split over workgroups and the workspace, never the result's validity.  The workspace for max_kv 0
+ * (any length) is enough for every max_kv.
+ * The cache's dtype is that of q or VQ_E4M3; head_dim 64 or 128.  Scores, softmax statistics and sums are
+ * fp32; the probabilities enter the second product rounded to q's dtype.
+ * Limits (SHAPE): tokens <= 2^22, tokens * q_heads <= 2^26, seqs * cache->heads <= 2^21, table_cols * page_size <= 2^30.
+ * Errors: NULL, SHAPE, BITS, STRIDE, STEP (scale not finite), UNSUPPORTED, WORKSPACE.
+ */
+vq_status vq_attention_paged_workspace(int64_t tokens, int32_t seqs, int32_t q_heads,
+                                       const vq_kv_cache *cache, int64_t max_kv, size_t *bytes);
+vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64_t q_ld, int32_t q_heads,
+                             const int32_t *q_offsets, const int32_t *kv_lens, int32_t seqs,
+                             const int32_t *page_table, int64_t table_stride, int32_t table_cols,
+                             const vq_kv_cache *cache, float scale, int32_t causal, int32_t window,
+                             int64_t max_kv, void *out, int64_t out_ld, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 /*
  * Measurement aid (not part of the method): enqueues a register-resident loop of the int8 matrix
  * instruction the linears run on (v_mfma_i32_32x32x32_i8, operands of the kind the kernels feed,

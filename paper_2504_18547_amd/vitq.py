@@ -20,7 +20,11 @@ EXPORTS = ["vq_status_string", "vq_weight_steps", "vq_quantize", "vq_linear", "v
            "vq_prepack_weight_bytes", "vq_prepack_weight", "vq_linear_prepacked", "vq_layernorm_quantize",
            "vq_vit_block_workspace", "vq_vit_block", "vq_qkv_headnorm", "vq_absorb_thresholds",
            "vq_linear_absorbed", "vq_recode_e3m2_bytes", "vq_recode_e3m2", "vq_linear_e3m2", "vq_vit_encoder_workspace", "vq_vit_encoder", "vq_attention_block_static", "vq_probe_mfma_i8",
-           "vq_probe_gelu_distance"]
+           "vq_probe_gelu_distance", "vq_quantize_e4m3", "vq_linear_e4m3", "vq_qkv_norm_rotate",
+           "vq_attention_paged_workspace", "vq_attention_paged"]
+
+VQ_F32, VQ_BF16, VQ_F16, VQ_E4M3 = range(4)
+_DTYPES = {torch.float32: VQ_F32, torch.bfloat16: VQ_BF16, torch.float16: VQ_F16, torch.float8_e4m3fn: VQ_E4M3}
 
 
 class VitqError(RuntimeError):
@@ -58,6 +62,25 @@ class vq_preln_desc(C.Structure):
     _fields_ = [("block", vq_block_desc), ("ln1_gamma", C.c_void_p), ("ln1_beta", C.c_void_p),
                 ("ln2_gamma", C.c_void_p), ("ln2_beta", C.c_void_p), ("ln_eps", C.c_float),
                 ("reserved", C.c_int32), ("dump_xq", C.c_void_p), ("dump_x1", C.c_void_p)]
+
+
+class vq_fmat(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p), ("block_rows", C.c_int32), ("reserved", C.c_int32),
+                ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+
+class vq_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32), ("heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("pages", C.c_int64), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("token_stride", C.c_int64), ("k_scale", C.c_float), ("v_scale", C.c_float)]
+
+
+class vq_rotate_desc(C.Structure):
+    _fields_ = [("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("norm", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("q_gamma", C.c_void_p), ("q_beta", C.c_void_p),
+                ("k_gamma", C.c_void_p), ("k_beta", C.c_void_p), ("gamma_head_stride", C.c_int64),
+                ("cos_table", C.c_void_p), ("sin_table", C.c_void_p), ("table_rows", C.c_int64), ("eps", C.c_float),
+                ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -105,6 +128,14 @@ def lib():
         _lib.vq_vit_block.argtypes = [C.POINTER(vq_preln_desc), vp, C.c_int64, vp, vp, C.c_size_t, vp]
         _lib.vq_vit_encoder_workspace.argtypes = [C.POINTER(vq_preln_desc), C.c_int32, C.c_int64, C.POINTER(C.c_size_t)]
         _lib.vq_vit_encoder.argtypes = [C.POINTER(vq_preln_desc), C.c_int32, vp, C.c_int64, vp, vp, C.c_size_t, vp]
+        fp, i32, i64 = C.POINTER(vq_fmat), C.c_int32, C.c_int64
+        cp = C.POINTER(vq_kv_cache)
+        _lib.vq_quantize_e4m3.argtypes = [vp, i32, i64, i64, i64, fp, vp]
+        _lib.vq_linear_e4m3.argtypes = [fp, fp, vp, i32, vp, i32, i64, vp]
+        _lib.vq_qkv_norm_rotate.argtypes = [C.POINTER(vq_rotate_desc), vp, i32, i64, i64, vp, vp, i32, i64, cp, vp, vp]
+        _lib.vq_attention_paged_workspace.argtypes = [i64, i32, i32, cp, i64, C.POINTER(C.c_size_t)]
+        _lib.vq_attention_paged.argtypes = [vp, i32, i64, i64, i32, vp, vp, i32, vp, i64, i32, cp, C.c_float, i32, i32,
+                                            i64, vp, i64, vp, vp, C.c_size_t, vp]
         for n in EXPORTS[1:]:
             getattr(_lib, n).restype = C.c_int
     return _lib
@@ -376,3 +407,164 @@ def vq_vit_encoder(descs, x, B, y_out, workspace):
     _check(lib().vq_vit_encoder(_layer_array(descs), len(descs), _ptr(x), int(B), _ptr(y_out), _ptr(workspace),
                                 workspace.numel() * workspace.element_size() if workspace is not None else 0,
                                 _stream()), "vq_vit_encoder")
+
+
+# ---- operators of the serving layer ------------------------------------------------------------------------
+
+def _want(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _here(*tensors):
+    """Device pointers go to the library: every tensor has to be on the current device, whose stream the call takes."""
+    current = _current_device() if _current_device is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError("tensor on %s, but the current device is cuda:%d" % (t.device, current))
+
+
+def _rows_2d(t, what):
+    """(dtype code, leading dimension) of a tensor [rows, cols] whose rows are contiguous."""
+    _want(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), what + " must be [rows, cols] with contiguous rows")
+    _want(t.dtype in _DTYPES, what + " has a type the library does not take")
+    ld = t.stride(0)
+    return _DTYPES[t.dtype], (ld if t.shape[0] > 1 else max(ld, t.shape[1]))
+
+
+def _vector(t, dtype, count, what):
+    if t is not None:
+        _want(t.dtype == dtype and t.dim() == 1 and t.is_contiguous() and (count is None or t.shape[0] == count),
+              "%s must be a contiguous %s vector%s" % (what, dtype, "" if count is None else " of %d" % count))
+    return t
+
+
+class FMat:
+    """A matrix of E4M3 codes with fp32 block scales: data uint8 [rows, row_stride], scales [ceil(cols/128), scale_stride],
+    one per 128 columns and block_rows (1: activations, 128: weights) rows."""
+
+    def __init__(self, data, scales, cols, block_rows):
+        _want(data.dtype == torch.uint8 and data.dim() == 2 and data.is_contiguous(), "data must be contiguous uint8 [rows, row_stride]")
+        _want(scales.dtype == torch.float32 and scales.dim() == 2 and scales.is_contiguous(), "scales must be contiguous fp32 [column blocks, row blocks]")
+        self.data, self.scales = data, scales
+        self.rows, self.row_stride = data.shape
+        self.cols, self.block_rows = int(cols), int(block_rows)
+        _want(scales.shape[0] >= (self.cols + 127) // 128, "scales must hold a row for every 128 columns")
+        self._c = vq_fmat(data.data_ptr() or None, scales.data_ptr() or None, self.block_rows, 0, self.rows, self.cols,
+                          self.row_stride, scales.shape[1])
+        self._ref = C.byref(self._c)
+
+    @staticmethod
+    def empty(rows, cols, block_rows=1, device="cuda"):
+        data = torch.zeros((rows, (cols + 15) // 16 * 16), dtype=torch.uint8, device=device)
+        blocks = (rows + block_rows - 1) // block_rows
+        return FMat(data, torch.zeros(((cols + 127) // 128, blocks), dtype=torch.float32, device=device), cols, block_rows)
+
+    def c(self):
+        return self._c
+
+
+class KvCache:
+    """A paged cache over the caller's k and v, both seen as [page, head, place in the page, channel] (a permuted view where
+    the memory has tokens first): bfloat16, float16, or float8_e4m3fn with the scale of a code unit."""
+
+    def __init__(self, k, v, k_scale=1.0, v_scale=1.0):
+        _want(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device and k.stride() == v.stride(),
+              "k and v must be [pages, heads, page_size, head_dim] alike")
+        _want(k.dtype in _DTYPES and k.stride(3) == 1, "channels must be contiguous, of a type the library takes")
+        self.k, self.v = k, v
+        pages, heads, page_size, head_dim = k.shape
+        self._c = vq_kv_cache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], heads, head_dim, page_size, pages, k.stride(0),
+                              k.stride(1), k.stride(2), float(k_scale), float(v_scale))
+        self._ref = C.byref(self._c)
+
+    def c(self):
+        return self._c
+
+
+def vq_quantize_e4m3(x, out):
+    code, ld = _rows_2d(x, "x")
+    _here(x, out.data, out.scales)
+    _check(lib().vq_quantize_e4m3(x.data_ptr(), code, x.shape[0], x.shape[1], ld, out._ref, _stream()), "vq_quantize_e4m3")
+    return out
+
+
+def vq_linear_e4m3(x, w, bias, act, y):
+    code, ld = _rows_2d(y, "y")
+    _want(y.shape[0] == x.rows and y.shape[1] == w.rows, "y must be [rows of x, rows of w]")
+    _vector(bias, torch.float32, w.rows, "bias")
+    _here(x.data, w.data, bias, y)
+    _check(lib().vq_linear_e4m3(x._ref, w._ref, _ptr(bias), int(act), y.data_ptr(), code, ld, _stream()), "vq_linear_e4m3")
+
+
+_NORMS = {"none": 0, "rms": 1, "layer": 2}
+
+
+def make_rotate_desc(q_heads, kv_heads, head_dim, norm="rms", q_gamma=None, q_beta=None, k_gamma=None, k_beta=None, eps=1e-6,
+                     cos=None, sin=None, interleaved=False):
+    """norm: "none", "rms" or "layer"; gammas and betas [head_dim] or, all of them, [heads, head_dim]; cos, sin: tables
+    [rows, rot_dim/2] or None.  The descriptor keeps the tensors alive."""
+    d = vq_rotate_desc()
+    d.q_heads, d.kv_heads, d.head_dim = q_heads, kv_heads, head_dim
+    d.norm, d.eps, d.interleaved = _NORMS[norm], float(eps), int(interleaved)
+    given = [("q_gamma", q_gamma, q_heads), ("q_beta", q_beta, q_heads), ("k_gamma", k_gamma, kv_heads), ("k_beta", k_beta, kv_heads)]
+    per_head = any(t is not None and t.dim() == 2 for _, t, _ in given)
+    for name, t, heads in given:
+        if t is not None:
+            _want(t.dtype == torch.float32 and t.is_contiguous(), name + " must be contiguous fp32")
+            _want(tuple(t.shape) == ((heads, head_dim) if per_head else (head_dim,)), name + " has the wrong shape")
+            setattr(d, name, t.data_ptr())
+    d.gamma_head_stride = head_dim if per_head else 0
+    _want((cos is None) == (sin is None), "cos and sin go together")
+    if cos is not None:
+        for t in (cos, sin):
+            _want(t.dtype == torch.float32 and t.dim() == 2 and t.is_contiguous() and t.shape == cos.shape, "cos and sin must be contiguous fp32 [rows, rot_dim/2]")
+        d.cos_table, d.sin_table, d.table_rows, d.rot_dim = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1]
+    d._keep = (q_gamma, q_beta, k_gamma, k_beta, cos, sin)
+    d._ref = C.byref(d)
+    return d
+
+
+def vq_qkv_norm_rotate(desc, qkv, positions, q_out, cache, slots):
+    code, ld = _rows_2d(qkv, "qkv")
+    tokens = qkv.shape[0]
+    _want(qkv.shape[1] == (desc.q_heads + 2 * desc.kv_heads) * desc.head_dim, "qkv must have a column per channel of every head")
+    _vector(positions, torch.int32, tokens, "positions")
+    _vector(slots, torch.int64, tokens, "slots")
+    q_code, q_ld = 0, 0
+    if q_out is not None:
+        q_code, q_ld = _rows_2d(q_out, "q_out")
+        _want(q_out.shape[0] == tokens and q_out.shape[1] == desc.q_heads * desc.head_dim, "q_out must be [tokens, q_heads*head_dim]")
+    _here(qkv, positions, q_out, slots, None if cache is None else cache.k, *desc._keep)
+    _check(lib().vq_qkv_norm_rotate(desc._ref, qkv.data_ptr(), code, tokens, ld, _ptr(positions), _ptr(q_out), q_code, q_ld,
+                                    None if cache is None else cache._ref, _ptr(slots), _stream()), "vq_qkv_norm_rotate")
+
+
+def vq_attention_paged_workspace(tokens, seqs, q_heads, cache, max_kv):
+    """Bytes that vq_attention_paged needs; max_kv as there (0 there: table columns * page size here)."""
+    n = C.c_size_t()
+    _check(lib().vq_attention_paged_workspace(int(tokens), int(seqs), int(q_heads), cache._ref, int(max_kv), C.byref(n)),
+           "vq_attention_paged_workspace")
+    return n.value
+
+
+def vq_attention_paged(q, q_offsets, kv_lens, page_table, cache, scale, causal, window, max_kv, out, lse, workspace):
+    code, ld = _rows_2d(q, "q")
+    out_code, out_ld = _rows_2d(out, "out")
+    tokens, cols = q.shape
+    _want(out.shape == q.shape and out_code == code, "out must be like q")
+    _want(cols % cache._c.head_dim == 0, "q must have a column per channel of every head")
+    q_heads = cols // cache._c.head_dim
+    _vector(kv_lens, torch.int32, None, "kv_lens")
+    seqs = kv_lens.shape[0]
+    _vector(q_offsets, torch.int32, seqs + 1, "q_offsets")
+    _want(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == seqs
+          and (page_table.stride(1) == 1 or page_table.shape[1] <= 1), "page_table must be int32 [sequences, pages] with contiguous rows")
+    if lse is not None:
+        _want(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (tokens, q_heads), "lse must be contiguous fp32 [tokens, q_heads]")
+    _here(q, q_offsets, kv_lens, page_table, cache.k, out, lse, workspace)
+    _check(lib().vq_attention_paged(q.data_ptr(), code, tokens, ld, q_heads, q_offsets.data_ptr(), kv_lens.data_ptr(), seqs,
+                                    page_table.data_ptr(), max(page_table.stride(0), page_table.shape[1]), page_table.shape[1], cache._ref, float(scale), int(causal),
+                                    int(window), int(max_kv), out.data_ptr(), out_ld, _ptr(lse), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()),
+           "vq_attention_paged")
