@@ -6,6 +6,8 @@
 // (rows = channels), B operand = tokens (columns): a lane then holds ONE token, so its scale product is one value per token
 // tile, and four consecutive channels, which leave as one store.
 #include "gemm_e4m3.h"
+
+#include "launch_util.h"
 #include "serve_dev.h"
 
 namespace vitq {
@@ -21,8 +23,8 @@ template <bool WIDE>
 __device__ __forceinline__ v4f mfma_block(const v8i &w, const v8i &x) {
     v4f c = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     if constexpr (!WIDE) {
-        // formats 0 / 0: E4M3 on both sides; the constant scale 127 is the exponent of 1
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+        // formats 0 / 0: E4M3 on both sides; constant zero scales select the instruction without them
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) c = mfma16<kBF16>(widen8<kBF16>((u32)w[2 * i], (u32)w[2 * i + 1]), widen8<kBF16>((u32)x[2 * i], (u32)x[2 * i + 1]), c);
@@ -43,9 +45,11 @@ __device__ __forceinline__ void store4(const GemmE4M3Params &p, int m, int n, v4
     if (p.y_dtype == kF32) {
         float *d = reinterpret_cast<float *>(p.y) + at;
         if (p.vec_ok && valid >= 4) *reinterpret_cast<v4f *>(d) = y;
-        else
+        else {
+#pragma unroll
             for (int r = 0; r < 4; ++r)
                 if (r < valid) d[r] = y[r];
+        }
     } else {
         uint2 w;
         if (p.y_dtype == kBF16) { w.x = pack_bf16(y[0], y[1]); w.y = pack_bf16(y[2], y[3]); }
@@ -167,10 +171,198 @@ hipError_t launch_split(const GemmE4M3Params &p, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// ---- many tiles: operands through LDS ------------------------------------------------------------------------------------
+// A workgroup of WC x WT waves owns WC*AT*16 channels x WT*TT*16 tokens; a stage is one block of the contraction (128 bytes of
+// every row and the tokens' scales), two stages in LDS, filled by loads that go straight there.  LDS rows are unpadded, their
+// 16-byte chunks permuted by the row so that the sixteen rows of an operand spread over the banks; weight rows sit in an order
+// that gives a lane sixteen consecutive channels over four channel tiles.
+__device__ __forceinline__ u32 lds_address_of(const void *p) {
+    return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p;
+}
+// Loads straight to LDS through a buffer descriptor: lane i's 16 (4) bytes at byte `off` go to dst + 16 i (4 i), zeros where
+// `off` lies beyond the descriptor's size.  The compiler does not see them; they are waited for with vmcnt by hand.
+__device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ v4i descriptor(uint64_t base, u32 bytes) {
+    v4i d;
+    d[0] = (int)uniform((u32)base); d[1] = (int)uniform((u32)(base >> 32)); d[2] = (int)uniform(bytes); d[3] = 0x00020000;
+    return d;
+}
+// `rows` rows (none if not positive) of `stride` bytes, the last one `tail` bytes long
+__device__ __forceinline__ v4i rows_descriptor(uint64_t base, int rows, u32 stride, u32 tail) {
+    return descriptor(base, rows > 0 ? (u32)(rows - 1) * stride + tail : 0u);
+}
+__device__ __forceinline__ void to_lds16(u32 off, const v4i &buf, u32 dst) {
+    u32 keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep) : "v"(off), "s"(buf), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void to_lds4(u32 off, const v4i &buf, u32 dst) {
+    u32 keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep) : "v"(off), "s"(buf), "s"(dst) : "memory");
+}
+
+template <bool WIDE, int WC, int WT, int AT, int TT>
+__global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const GemmE4M3Params p) {
+    constexpr int kThreads = WC * WT * 64;
+    constexpr int TC = WC * AT * 16, TK = WT * TT * 16;              // channels, tokens of the tile
+    constexpr int kStage = (TC + TK) * 128 + TK * 4;
+    static_assert((TC * 8) % kThreads == 0 && (TK * 8) % kThreads == 0, "a load instruction takes rows of one operand");
+    static_assert(TK <= kThreads && TK % 64 == 0, "one scale load per wave");
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wc = wave % WC, wt = wave / WC;
+    const int l16 = lane & 15, q = lane >> 4;
+
+    // Workgroups go round-robin to the eight XCDs: give each XCD a run of consecutive tiles, walked in strips of four token
+    // tiles, so that the workgroups of one L2 share operand rows.
+    const int n_ct = (p.Nout + TC - 1) / TC, n_tt = (p.M + TK - 1) / TK;
+    int id;
+    {
+        const int total = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+        const int per = total >> 3, rem = total & 7;
+        id = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + slot;
+    }
+    const int strip = id / (4 * n_ct), in_strip = id - strip * 4 * n_ct;
+    const int height = min(4, n_tt - 4 * strip);
+    // (the divisions run on the vector unit: back to scalars, and with them every address that follows)
+    const int col = (int)uniform((u32)(in_strip / height)), c0 = col * TC;
+    const int t0 = ((int)uniform((u32)(4 * strip + in_strip)) - col * (int)uniform((u32)height)) * TK;
+    const int nk = (p.K + 127) >> 7;
+
+    // What each lane fetches per stage: chunk `chunk` of the rows r0 + kStep*i of the weights, then of the tokens.  LDS row r of
+    // the weights is channel 64*(r/64) + 16*((r/4)%4) + 4*((r/16)%4) + r%4 of the tile: a lane's results of four channel tiles
+    // are then sixteen consecutive channels.  Rows beyond the matrix and chunks beyond a ragged K arrive as zeros.
+    constexpr int kStep = kThreads / 8, kLoadsW = TC / kStep, kLoadsX = TK / kStep;
+    static_assert(TC % kStep == 0 && TK % kStep == 0 && (kStep == 64 || kStep == 32), "rows per load instruction");
+    const int r0 = (int)threadIdx.x >> 3;
+    const u32 chunk = (u32)((threadIdx.x & 7) ^ (r0 & 7)) * 16u;
+    const int rows_w = min(TC, p.Nout - c0), rows_x = min(TK, p.M - t0);
+    const uint64_t wbase = (uint64_t)(uintptr_t)p.w + (uint64_t)c0 * p.w_stride, xbase = (uint64_t)(uintptr_t)p.x + (uint64_t)t0 * p.x_stride;
+    const u32 w_stride = (u32)p.w_stride, x_stride = (u32)p.x_stride;
+    const u32 lds0 = __builtin_amdgcn_readfirstlane(lds_address_of(smem));
+    const u32 woff = (u32)(64 * (r0 >> 6) + 16 * ((r0 >> 2) & 3) + 4 * ((r0 >> 4) & 3) + (r0 & 3)) * w_stride + chunk;
+    const u32 xoff = (u32)r0 * x_stride + chunk;
+    auto issue = [&](int kt) {
+        const u32 stage = lds0 + (u32)(kt & 1) * kStage;
+        const u32 dst = stage + (u32)wave * 1024u;
+        const bool in = kt * 128 + (int)chunk < p.kbytes16;
+        const u32 wk = in ? woff + (u32)kt * 128u : ~15u, xk = in ? xoff + (u32)kt * 128u : ~15u;
+        // (channels of the rows kStep*i further: 64 per 64 rows; 32 rows are two channel tiles, 8 channels)
+#pragma unroll
+        for (int i = 0; i < kLoadsW; ++i) {
+            const u32 step = kStep == 64 ? 64 * i : 64 * (i >> 1) + 8 * (i & 1);
+            to_lds16(wk, rows_descriptor(wbase + step * w_stride, rows_w - (int)step, w_stride, p.kbytes16), dst + i * (kThreads * 16));
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsX; ++i)
+            to_lds16(xk, rows_descriptor(xbase + (u32)(kStep * i) * x_stride, rows_x - kStep * i, x_stride, p.kbytes16), dst + (kLoadsW + i) * (kThreads * 16));
+        if (wave * 64 < TK)
+            to_lds4(threadIdx.x * 4u, descriptor((uint64_t)(uintptr_t)(p.xs + (int64_t)kt * p.xs_stride + t0), (u32)rows_x * 4u), stage + (TC + TK) * 128 + wave * 256);
+    };
+    // (read-only for the whole kernel: scalar loads)
+    const __attribute__((address_space(4))) float *wsc =
+        (const __attribute__((address_space(4))) float *)(uintptr_t)(p.ws + (min(c0 + wc * (16 * AT), p.Nout - 1) >> 7));
+
+    v4f acc[AT][TT];
+#pragma unroll
+    for (int a = 0; a < AT; ++a)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[a][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    issue(0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (nk > 1) issue(1);
+
+    // byte offsets of this lane's two chunks inside a row, and of its rows inside a stage
+    const u32 p0 = (u32)((q ^ (l16 & 7)) * 16), p1 = (u32)(((q + 4) ^ (l16 & 7)) * 16);
+    const u32 wrow = (u32)((wc * (16 * AT) + l16) * 128), xrow = (u32)((TC + wt * (16 * TT) + l16) * 128);
+    auto frag = [&](const uint8_t *stage, u32 row) {
+        return operand(*reinterpret_cast<const uint4 *>(stage + row + p0), *reinterpret_cast<const uint4 *>(stage + row + p1));
+    };
+    v8i xf[TT], wf[2];
+    float sc[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) xf[t] = frag(smem, xrow + t * 2048);
+    wf[0] = frag(smem, wrow);
+    float sw = wsc[0];
+    // Products run kLag ahead of the FMAs that add them to the totals, so that neither waits for the other.
+    constexpr int kLag = 3;
+    v4f d[kLag + 1];
+    auto add = [&](int i) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i / TT][i % TT][r] = fmaf(d[i % (kLag + 1)][r], sc[i % TT], acc[i / TT][i % TT][r]);
+        asm volatile("" : "+v"(acc[i / TT][i % TT]));           // here, not later: the products' registers are needed again
+    };
+    for (int kt = 0; kt < nk; ++kt) {
+        const uint8_t *stage = smem + (kt & 1) * kStage;
+        const uint8_t *next = smem + ((kt + 1) & 1) * kStage;
+        const float *xs = reinterpret_cast<const float *>(stage + (TC + TK) * 128) + wt * (16 * TT) + l16;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) sc[t] = xs[16 * t] * sw;
+        if (kt + 1 < nk) sw = wsc[(int64_t)(kt + 1) * p.ws_stride];
+        static_for<AT * TT>([&](auto I) {
+            constexpr int i = decltype(I)::value, a = i / TT, t = i % TT;
+            if constexpr (t == 0) {
+                if constexpr (a + 1 < AT) {
+                    wf[(a + 1) & 1] = frag(stage, wrow + (a + 1) * 2048);
+                } else {
+                    // every operand of this stage is in registers: its buffer is free once all waves say so, the other is full
+                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    if (kt + 2 < nk) issue(kt + 2);
+                    wf[0] = frag(next, wrow);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            d[i % (kLag + 1)] = mfma_block<WIDE>(wf[a & 1], xf[t]);
+            if constexpr (a + 1 == AT) {
+                xf[t] = frag(next, xrow + t * 2048);      // (behind the last stage: read, never used)
+            }
+            if constexpr (i >= kLag) add(i - kLag);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        static_for<kLag>([&](auto I) { add(AT * TT - kLag + decltype(I)::value); });
+    }
+
+    // a lane's sixteen consecutive channels of one token per four channel tiles
+#pragma unroll
+    for (int g = 0; g < AT / 4; ++g) {
+        const int n = c0 + wc * (16 * AT) + 64 * g + 16 * q;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const int m = t0 + wt * (16 * TT) + 16 * t + l16;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) store4(p, m, n + 4 * j, acc[4 * g + j][t]);
+        }
+    }
+}
+
+template <bool WIDE, int WC, int WT, int AT, int TT>
+hipError_t launch_tile(const GemmE4M3Params &p, hipStream_t stream) {
+    constexpr int TC = WC * AT * 16, TK = WT * TT * 16;
+    constexpr int lds = 2 * ((TC + TK) * 128 + TK * 4);
+    static std::atomic<uint64_t> done{0};
+    auto kern = gemm_e4m3_tile_kernel<WIDE, WC, WT, AT, TT>;
+    hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds, done);
+    if (e != hipSuccess) return e;
+    const int64_t tiles = (int64_t)((p.Nout + TC - 1) / TC) * ((p.M + TK - 1) / TK);
+    hipLaunchKernelGGL(kern, dim3((u32)tiles), dim3(WC * WT * 64), lds, stream, p);
+    return hipGetLastError();
+}
+
 template <bool WIDE>
 hipError_t launch(const GemmE4M3Params &p, hipStream_t stream) {
+    const int64_t blocks = (int64_t)((p.M + 31) / 32) * ((p.Nout + 31) / 32);
     if (p.M <= 16) return launch_split<WIDE, 1, 1, 4>(p, stream);
-    return launch_split<WIDE, 2, 2, 1>(p, stream);
+    if (blocks <= 1000) return launch_split<WIDE, 2, 2, 1>(p, stream);
+    const int64_t big = (int64_t)((p.M + 255) / 256) * ((p.Nout + 255) / 256);
+    if (big >= 192) return launch_tile<WIDE, 2, 4, 8, 4>(p, stream);
+    return launch_tile<WIDE, 2, 2, 4, 4>(p, stream);
 }
 
 }  // namespace
