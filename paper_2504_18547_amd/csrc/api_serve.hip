@@ -118,7 +118,7 @@ vq_status vq_linear_e4m3(const vq_fmat *x, const vq_fmat *w, const float *bias, 
     p.w = (const uint8_t *)w->data; p.w_stride = w->row_stride; p.ws = w->scales; p.ws_stride = w->scale_stride; p.Nout = (int)w->rows;
     p.K = (int)x->cols; p.kbytes16 = (int)((x->cols + 15) / 16 * 16);
     p.bias = bias; p.act = act; p.y = y; p.y_dtype = y_dtype; p.ld = ld;
-    p.vec_ok = ((uintptr_t)y) % (4 * size) == 0 && ld % 4 == 0;
+    p.vec_ok = aligned16(y) && (ld * size) % 16 == 0;
     return vitq::gemm_e4m3_launch(p, (hipStream_t)stream) == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 

@@ -12,7 +12,7 @@ struct GemmE4M3Params {
     int kbytes16;                 // bytes of a row up to its padding
     const float *bias; int act;
     void *y; int y_dtype; int64_t ld;
-    int vec_ok;                   // four consecutive outputs of a row are one aligned store
+    int vec_ok;                   // rows of y are 16-byte aligned
 };
 hipError_t gemm_e4m3_launch(const GemmE4M3Params &p, hipStream_t stream);
 

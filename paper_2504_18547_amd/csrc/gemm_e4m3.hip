@@ -65,6 +65,31 @@ __device__ __forceinline__ void store4(const GemmE4M3Params &p, int m, int n, v4
     }
 }
 
+// Eight consecutive outputs n.. of token m; full: all of them exist and are aligned for whole stores.
+__device__ __forceinline__ void store8_f32(const GemmE4M3Params &p, int m, int n, const float (&y)[8], bool full) {
+    float *d = reinterpret_cast<float *>(p.y) + (int64_t)m * p.ld + n;
+    if (full) {
+        reinterpret_cast<v4f *>(d)[0] = v4f{y[0], y[1], y[2], y[3]};
+        reinterpret_cast<v4f *>(d)[1] = v4f{y[4], y[5], y[6], y[7]};
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (n + j < p.Nout) d[j] = y[j];
+    }
+}
+__device__ __forceinline__ void store8_16bit(const GemmE4M3Params &p, int m, int n, const float (&y)[8], bool full) {
+    u32 w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = p.y_dtype == kBF16 ? pack_bf16(y[2 * j], y[2 * j + 1]) : pack_f16(y[2 * j], y[2 * j + 1]);
+    uint16_t *d = reinterpret_cast<uint16_t *>(p.y) + (int64_t)m * p.ld + n;
+    if (full) *reinterpret_cast<uint4 *>(d) = make_uint4(w[0], w[1], w[2], w[3]);
+    else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (n + j < p.Nout) d[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+}
+
 __device__ __forceinline__ v8i operand(const uint4 &a, const uint4 &b) {
     v8i r;
     r[0] = (int)a.x; r[1] = (int)a.y; r[2] = (int)a.z; r[3] = (int)a.w;
@@ -242,25 +267,28 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     const uint64_t wbase = (uint64_t)(uintptr_t)p.w + (uint64_t)c0 * p.w_stride, xbase = (uint64_t)(uintptr_t)p.x + (uint64_t)t0 * p.x_stride;
     const u32 w_stride = (u32)p.w_stride, x_stride = (u32)p.x_stride;
     const u32 lds0 = __builtin_amdgcn_readfirstlane(lds_address_of(smem));
-    const u32 woff = (u32)(64 * (r0 >> 6) + 16 * ((r0 >> 2) & 3) + 4 * ((r0 >> 4) & 3) + (r0 & 3)) * w_stride + chunk;
+    const u32 woff = (u32)(32 * (r0 >> 5) + 8 * ((r0 >> 2) & 3) + 4 * ((r0 >> 4) & 1) + (r0 & 3)) * w_stride + chunk;
     const u32 xoff = (u32)r0 * x_stride + chunk;
-    auto issue = [&](int kt) {
+    // part i of a stage's loads; part kLoadsW + kLoadsX: the tokens' scales
+    auto issue = [&](int kt, auto I) {
+        constexpr int i = decltype(I)::value;
         const u32 stage = lds0 + (u32)(kt & 1) * kStage;
-        const u32 dst = stage + (u32)wave * 1024u;
+        const u32 dst = stage + (u32)wave * 1024u + i * (kThreads * 16);
         const bool in = kt * 128 + (int)chunk < p.kbytes16;
-        const u32 wk = in ? woff + (u32)kt * 128u : ~15u, xk = in ? xoff + (u32)kt * 128u : ~15u;
-        // (channels of the rows kStep*i further: 64 per 64 rows; 32 rows are two channel tiles, 8 channels)
-#pragma unroll
-        for (int i = 0; i < kLoadsW; ++i) {
-            const u32 step = kStep == 64 ? 64 * i : 64 * (i >> 1) + 8 * (i & 1);
-            to_lds16(wk, rows_descriptor(wbase + step * w_stride, rows_w - (int)step, w_stride, p.kbytes16), dst + i * (kThreads * 16));
-        }
-#pragma unroll
-        for (int i = 0; i < kLoadsX; ++i)
-            to_lds16(xk, rows_descriptor(xbase + (u32)(kStep * i) * x_stride, rows_x - kStep * i, x_stride, p.kbytes16), dst + (kLoadsW + i) * (kThreads * 16));
-        if (wave * 64 < TK)
+        if constexpr (i < kLoadsW) {
+            constexpr int step = kStep * i;
+            to_lds16(in ? woff + (u32)kt * 128u : ~15u, rows_descriptor(wbase + (u32)step * w_stride, rows_w - step, w_stride, p.kbytes16), dst);
+        } else if constexpr (i < kLoadsW + kLoadsX) {
+            constexpr int step = kStep * (i - kLoadsW);
+            to_lds16(in ? xoff + (u32)kt * 128u : ~15u, rows_descriptor(xbase + (u32)step * x_stride, rows_x - step, x_stride, p.kbytes16), dst);
+        } else if (wave * 64 < TK) {
             to_lds4(threadIdx.x * 4u, descriptor((uint64_t)(uintptr_t)(p.xs + (int64_t)kt * p.xs_stride + t0), (u32)rows_x * 4u), stage + (TC + TK) * 128 + wave * 256);
+        }
     };
+    constexpr int kParts = kLoadsW + kLoadsX + 1;
+    // The first parts go out when the buffer is free, the others one per channel tile: a burst of all of them queues in the
+    // CU's one address path and holds the waves up.
+    constexpr int kFirst = kParts - (AT - 2) > 2 ? kParts - (AT - 2) : 2;
     // (read-only for the whole kernel: scalar loads)
     const __attribute__((address_space(4))) float *wsc =
         (const __attribute__((address_space(4))) float *)(uintptr_t)(p.ws + (min(c0 + wc * (16 * AT), p.Nout - 1) >> 7));
@@ -271,11 +299,11 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[a][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
-    issue(0);
+    static_for<kParts>([&](auto I) { issue(0, I); });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (nk > 1) issue(1);
+    if (nk > 1) static_for<kFirst>([&](auto I) { issue(1, I); });
 
     // byte offsets of this lane's two chunks inside a row, and of its rows inside a stage
     const u32 p0 = (u32)((q ^ (l16 & 7)) * 16), p1 = (u32)(((q + 4) ^ (l16 & 7)) * 16);
@@ -283,11 +311,12 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     auto frag = [&](const uint8_t *stage, u32 row) {
         return operand(*reinterpret_cast<const uint4 *>(stage + row + p0), *reinterpret_cast<const uint4 *>(stage + row + p1));
     };
-    v8i xf[TT], wf[2];
+    v8i xf[TT], wf[3];
     float sc[TT];
 #pragma unroll
     for (int t = 0; t < TT; ++t) xf[t] = frag(smem, xrow + t * 2048);
     wf[0] = frag(smem, wrow);
+    wf[1] = frag(smem, wrow + 2048);
     float sw = wsc[0];
     // Products run kLag ahead of the FMAs that add them to the totals, so that neither waits for the other.
     constexpr int kLag = 3;
@@ -304,40 +333,60 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
 #pragma unroll
         for (int t = 0; t < TT; ++t) sc[t] = xs[16 * t] * sw;
         if (kt + 1 < nk) sw = wsc[(int64_t)(kt + 1) * p.ws_stride];
+        v8i next0, next1;
         static_for<AT * TT>([&](auto I) {
             constexpr int i = decltype(I)::value, a = i / TT, t = i % TT;
+            // channel tiles are read two ahead; tile j of the next stage is tile AT + j of this one
             if constexpr (t == 0) {
-                if constexpr (a + 1 < AT) {
-                    wf[(a + 1) & 1] = frag(stage, wrow + (a + 1) * 2048);
-                } else {
+                if constexpr (a + 2 < AT) {
+                    wf[(a + 2) % 3] = frag(stage, wrow + (a + 2) * 2048);
+                    if constexpr (kFirst + a < kParts) {
+                        if (kt + 1 < nk) issue(kt + 1, std::integral_constant<int, kFirst + a>{});
+                    }
+                } else if constexpr (a + 1 == AT) {
                     // every operand of this stage is in registers: its buffer is free once all waves say so, the other is full
                     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
-                    if (kt + 2 < nk) issue(kt + 2);
-                    wf[0] = frag(next, wrow);
+                    next0 = frag(next, wrow);
+                    next1 = frag(next, wrow + 2048);
+                    if (kt + 2 < nk) static_for<kFirst>([&](auto J) { issue(kt + 2, J); });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            d[i % (kLag + 1)] = mfma_block<WIDE>(wf[a & 1], xf[t]);
-            if constexpr (a + 1 == AT) {
-                xf[t] = frag(next, xrow + t * 2048);      // (behind the last stage: read, never used)
-            }
+            d[i % (kLag + 1)] = mfma_block<WIDE>(wf[a % 3], xf[t]);
+            if constexpr (a + 1 == AT) xf[t] = frag(next, xrow + t * 2048);      // (behind the last stage: read, never used)
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (i >= kLag) add(i - kLag);
             __builtin_amdgcn_sched_barrier(0);
         });
+        wf[0] = next0;
+        wf[1] = next1;
         static_for<kLag>([&](auto I) { add(AT * TT - kLag + decltype(I)::value); });
     }
 
-    // a lane's sixteen consecutive channels of one token per four channel tiles
+    // a lane's eight consecutive channels of one token per two channel tiles
 #pragma unroll
-    for (int g = 0; g < AT / 4; ++g) {
-        const int n = c0 + wc * (16 * AT) + 64 * g + 16 * q;
+    for (int g = 0; g < AT / 2; ++g) {
+        const int n = c0 + wc * (16 * AT) + 32 * g + 8 * q;
+        float b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = p.bias && n + j < p.Nout ? p.bias[n + j] : 0.0f;
+        const bool full = p.vec_ok && n + 8 <= p.Nout;
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             const int m = t0 + wt * (16 * TT) + 16 * t + l16;
+            float y[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) store4(p, m, n + 4 * j, acc[4 * g + j][t]);
+            for (int j = 0; j < 8; ++j) y[j] = acc[2 * g + (j >> 2)][t][j & 3] + b[j];
+            if (p.act) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] = gelu_fast(y[j]);
+            }
+            if (m < p.M) {
+                if constexpr (WIDE) store8_f32(p, m, n, y, full);
+                else store8_16bit(p, m, n, y, full);
+            }
         }
     }
 }
