@@ -217,14 +217,10 @@ __device__ __forceinline__ v4i rows_descriptor(uint64_t base, int rows, u32 stri
     return descriptor(base, rows > 0 ? (u32)(rows - 1) * stride + tail : 0u);
 }
 __device__ __forceinline__ void to_lds16(u32 off, const v4i &buf, u32 dst) {
-    u32 keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep) : "v"(off), "s"(buf), "s"(dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory", "m0");
 }
 __device__ __forceinline__ void to_lds4(u32 off, const v4i &buf, u32 dst) {
-    u32 keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep) : "v"(off), "s"(buf), "s"(dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory", "m0");
 }
 
 template <bool WIDE, int WC, int WT, int AT, int TT>
@@ -240,70 +236,81 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     const int wc = wave % WC, wt = wave / WC;
     const int l16 = lane & 15, q = lane >> 4;
 
-    // Workgroups go round-robin to the eight XCDs: give each XCD a run of consecutive tiles, walked in strips of four token
-    // tiles, so that the workgroups of one L2 share operand rows.
-    const int n_ct = (p.Nout + TC - 1) / TC, n_tt = (p.M + TK - 1) / TK;
-    int id;
-    {
-        const int total = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-        const int per = total >> 3, rem = total & 7;
-        id = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + slot;
-    }
-    const int strip = id / (4 * n_ct), in_strip = id - strip * 4 * n_ct;
-    const int height = min(4, n_tt - 4 * strip);
-    // (the divisions run on the vector unit: back to scalars, and with them every address that follows)
-    const int col = (int)uniform((u32)(in_strip / height)), c0 = col * TC;
-    const int t0 = ((int)uniform((u32)(4 * strip + in_strip)) - col * (int)uniform((u32)height)) * TK;
+    // The tiles in strips of four token tiles; workgroups go round-robin to the eight XCDs, each XCD has a run of consecutive
+    // tiles, so that the workgroups of one L2 share operand rows, and a workgroup every `stride`-th of its XCD's.
+    const int n_ct = (p.Nout + TC - 1) / TC, n_tt = (p.M + TK - 1) / TK, tiles = n_ct * n_tt;
+    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+    const int per = tiles >> 3, rem = tiles & 7;
+    const int run0 = xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per, run1 = run0 + per + (xcd < rem ? 1 : 0);
+    const int stride = ((int)gridDim.x + 7 - xcd) >> 3;               // workgroups of this XCD
     const int nk = (p.K + 127) >> 7;
+    auto place = [&](int id, int &c0, int &t0) {
+        const int strip = id / (4 * n_ct), in_strip = id - strip * 4 * n_ct;
+        const int height = min(4, n_tt - 4 * strip);
+        // (the divisions run on the vector unit: back to scalars, and with them every address that follows)
+        const int col = (int)uniform((u32)(in_strip / height));
+        c0 = col * TC;
+        t0 = ((int)uniform((u32)(4 * strip + in_strip)) - col * (int)uniform((u32)height)) * TK;
+    };
+    int id = run0 + slot;
+    if (id >= run1) return;
 
-    // What each lane fetches per stage: chunk `chunk` of the rows r0 + kStep*i of the weights, then of the tokens.  LDS row r of
-    // the weights is channel 64*(r/64) + 16*((r/4)%4) + 4*((r/16)%4) + r%4 of the tile: a lane's results of four channel tiles
-    // are then sixteen consecutive channels.  Rows beyond the matrix and chunks beyond a ragged K arrive as zeros.
+    // What each lane fetches per stage: chunk `chunk` of the rows r0 + kStep*i of the weights, then of the tokens.  LDS row r
+    // of the weights is channel 32*(r/32) + 8*((r/4)%4) + 4*((r/16)%2) + r%4 of the tile: a lane's results of two channel tiles
+    // are then eight consecutive channels.  Rows beyond the matrix and chunks beyond a ragged K arrive as zeros.
     constexpr int kStep = kThreads / 8, kLoadsW = TC / kStep, kLoadsX = TK / kStep;
     static_assert(TC % kStep == 0 && TK % kStep == 0 && (kStep == 64 || kStep == 32), "rows per load instruction");
     const int r0 = (int)threadIdx.x >> 3;
     const u32 chunk = (u32)((threadIdx.x & 7) ^ (r0 & 7)) * 16u;
-    const int rows_w = min(TC, p.Nout - c0), rows_x = min(TK, p.M - t0);
-    const uint64_t wbase = (uint64_t)(uintptr_t)p.w + (uint64_t)c0 * p.w_stride, xbase = (uint64_t)(uintptr_t)p.x + (uint64_t)t0 * p.x_stride;
     const u32 w_stride = (u32)p.w_stride, x_stride = (u32)p.x_stride;
-    const u32 lds0 = __builtin_amdgcn_readfirstlane(lds_address_of(smem));
+    const u32 lds0 = __builtin_amdgcn_readfirstlane(lds_address_of(smem)) + (u32)wave * 1024u;
     const u32 woff = (u32)(32 * (r0 >> 5) + 8 * ((r0 >> 2) & 3) + 4 * ((r0 >> 4) & 1) + (r0 & 3)) * w_stride + chunk;
     const u32 xoff = (u32)r0 * x_stride + chunk;
-    // part i of a stage's loads; part kLoadsW + kLoadsX: the tokens' scales
-    auto issue = [&](int kt, auto I) {
+
+    // The stages of all tiles of the workgroup are one sequence; the load cursor runs up to two stages ahead of the sums.
+    v4i wbuf[kLoadsW], xbuf[kLoadsX];
+    uint64_t sbase = 0;
+    u32 sbytes = 0;
+    int next_id = id, load_kt = 0;
+    auto point = [&](bool some) {                                    // descriptors of tile next_id (empty ones behind the last)
+        int c0 = 0, t0 = 0;
+        if (some) place(next_id, c0, t0);
+        const int rows_w = some ? min(TC, p.Nout - c0) : 0, rows_x = some ? min(TK, p.M - t0) : 0;
+        const uint64_t wbase = (uint64_t)(uintptr_t)p.w + (uint64_t)c0 * p.w_stride, xbase = (uint64_t)(uintptr_t)p.x + (uint64_t)t0 * p.x_stride;
+#pragma unroll
+        for (int i = 0; i < kLoadsW; ++i) wbuf[i] = rows_descriptor(wbase + (u32)(kStep * i) * w_stride, rows_w - kStep * i, w_stride, p.kbytes16);
+#pragma unroll
+        for (int i = 0; i < kLoadsX; ++i) xbuf[i] = rows_descriptor(xbase + (u32)(kStep * i) * x_stride, rows_x - kStep * i, x_stride, p.kbytes16);
+        sbase = (uint64_t)(uintptr_t)(p.xs + t0);
+        sbytes = (u32)rows_x * 4u;
+    };
+    // part i of the loads of the cursor's stage into buffer `half`; the last part: the tokens' scales
+    constexpr int kParts = kLoadsW + kLoadsX + 1;
+    auto issue = [&](int half, auto I) {
         constexpr int i = decltype(I)::value;
-        const u32 stage = lds0 + (u32)(kt & 1) * kStage;
-        const u32 dst = stage + (u32)wave * 1024u + i * (kThreads * 16);
-        const bool in = kt * 128 + (int)chunk < p.kbytes16;
-        if constexpr (i < kLoadsW) {
-            constexpr int step = kStep * i;
-            to_lds16(in ? woff + (u32)kt * 128u : ~15u, rows_descriptor(wbase + (u32)step * w_stride, rows_w - step, w_stride, p.kbytes16), dst);
-        } else if constexpr (i < kLoadsW + kLoadsX) {
-            constexpr int step = kStep * (i - kLoadsW);
-            to_lds16(in ? xoff + (u32)kt * 128u : ~15u, rows_descriptor(xbase + (u32)step * x_stride, rows_x - step, x_stride, p.kbytes16), dst);
-        } else if (wave * 64 < TK) {
-            to_lds4(threadIdx.x * 4u, descriptor((uint64_t)(uintptr_t)(p.xs + (int64_t)kt * p.xs_stride + t0), (u32)rows_x * 4u), stage + (TC + TK) * 128 + wave * 256);
+        const u32 dst = lds0 + (u32)half * kStage + i * (kThreads * 16);
+        const bool in = load_kt * 128 + (int)chunk < p.kbytes16;
+        if constexpr (i < kLoadsW) to_lds16(in ? woff + (u32)load_kt * 128u : ~15u, wbuf[i], dst);
+        else if constexpr (i < kLoadsW + kLoadsX) to_lds16(in ? xoff + (u32)load_kt * 128u : ~15u, xbuf[i - kLoadsW], dst);
+        else {
+            if (wave * 64 < TK)
+                to_lds4(threadIdx.x * 4u, descriptor(sbase + (uint64_t)load_kt * p.xs_stride * 4u, sbytes), lds0 - (u32)wave * 768u + (u32)half * kStage + (TC + TK) * 128);
+            if (++load_kt == nk) {
+                load_kt = 0;
+                next_id += stride;
+                point(next_id < run1);
+            }
         }
     };
-    constexpr int kParts = kLoadsW + kLoadsX + 1;
     // The first parts go out when the buffer is free, the others one per channel tile: a burst of all of them queues in the
     // CU's one address path and holds the waves up.
     constexpr int kFirst = kParts - (AT - 2) > 2 ? kParts - (AT - 2) : 2;
-    // (read-only for the whole kernel: scalar loads)
-    const __attribute__((address_space(4))) float *wsc =
-        (const __attribute__((address_space(4))) float *)(uintptr_t)(p.ws + (min(c0 + wc * (16 * AT), p.Nout - 1) >> 7));
-
-    v4f acc[AT][TT];
-#pragma unroll
-    for (int a = 0; a < AT; ++a)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) acc[a][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-
+    point(true);
     static_for<kParts>([&](auto I) { issue(0, I); });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (nk > 1) static_for<kFirst>([&](auto I) { issue(1, I); });
+    static_for<kFirst>([&](auto I) { issue(1, I); });
 
     // byte offsets of this lane's two chunks inside a row, and of its rows inside a stage
     const u32 p0 = (u32)((q ^ (l16 & 7)) * 16), p1 = (u32)(((q + 4) ^ (l16 & 7)) * 16);
@@ -317,22 +324,33 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     for (int t = 0; t < TT; ++t) xf[t] = frag(smem, xrow + t * 2048);
     wf[0] = frag(smem, wrow);
     wf[1] = frag(smem, wrow + 2048);
-    float sw = wsc[0];
     // Products run kLag ahead of the FMAs that add them to the totals, so that neither waits for the other.
     constexpr int kLag = 3;
-    v4f d[kLag + 1];
+    v4f d[kLag + 1], acc[AT][TT];
     auto add = [&](int i) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[i / TT][i % TT][r] = fmaf(d[i % (kLag + 1)][r], sc[i % TT], acc[i / TT][i % TT][r]);
         asm volatile("" : "+v"(acc[i / TT][i % TT]));           // here, not later: the products' registers are needed again
     };
+    int half = 0;
+    for (; id < run1; id += stride) {
+    int c0, t0;
+    place(id, c0, t0);
+    // (read-only for the whole kernel: scalar loads)
+    const __attribute__((address_space(4))) float *wsc =
+        (const __attribute__((address_space(4))) float *)(uintptr_t)(p.ws + (min(c0 + wc * (16 * AT), p.Nout - 1) >> 7));
+    float sw = wsc[0];
+#pragma unroll
+    for (int a = 0; a < AT; ++a)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[a][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     for (int kt = 0; kt < nk; ++kt) {
-        const uint8_t *stage = smem + (kt & 1) * kStage;
-        const uint8_t *next = smem + ((kt + 1) & 1) * kStage;
+        const uint8_t *stage = smem + half * kStage;
+        const uint8_t *next = smem + (half ^ 1) * kStage;
         const float *xs = reinterpret_cast<const float *>(stage + (TC + TK) * 128) + wt * (16 * TT) + l16;
 #pragma unroll
         for (int t = 0; t < TT; ++t) sc[t] = xs[16 * t] * sw;
-        if (kt + 1 < nk) sw = wsc[(int64_t)(kt + 1) * p.ws_stride];
+        sw = wsc[(int64_t)min(kt + 1, nk - 1) * p.ws_stride];
         v8i next0, next1;
         static_for<AT * TT>([&](auto I) {
             constexpr int i = decltype(I)::value, a = i / TT, t = i % TT;
@@ -340,9 +358,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
             if constexpr (t == 0) {
                 if constexpr (a + 2 < AT) {
                     wf[(a + 2) % 3] = frag(stage, wrow + (a + 2) * 2048);
-                    if constexpr (kFirst + a < kParts) {
-                        if (kt + 1 < nk) issue(kt + 1, std::integral_constant<int, kFirst + a>{});
-                    }
+                    if constexpr (kFirst + a < kParts) issue(half ^ 1, std::integral_constant<int, kFirst + a>{});
                 } else if constexpr (a + 1 == AT) {
                     // every operand of this stage is in registers: its buffer is free once all waves say so, the other is full
                     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -350,7 +366,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
                     asm volatile("" ::: "memory");
                     next0 = frag(next, wrow);
                     next1 = frag(next, wrow + 2048);
-                    if (kt + 2 < nk) static_for<kFirst>([&](auto J) { issue(kt + 2, J); });
+                    static_for<kFirst>([&](auto J) { issue(half, J); });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -363,6 +379,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
         wf[0] = next0;
         wf[1] = next1;
         static_for<kLag>([&](auto I) { add(AT * TT - kLag + decltype(I)::value); });
+        half ^= 1;
     }
 
     // a lane's eight consecutive channels of one token per two channel tiles
@@ -389,6 +406,9 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
             }
         }
     }
+    }
+    // the loads behind the last stage (zeros, into a buffer that nobody reads) land before the LDS is given back
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 template <bool WIDE, int WC, int WT, int AT, int TT>
@@ -400,7 +420,9 @@ hipError_t launch_tile(const GemmE4M3Params &p, hipStream_t stream) {
     hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds, done);
     if (e != hipSuccess) return e;
     const int64_t tiles = (int64_t)((p.Nout + TC - 1) / TC) * ((p.M + TK - 1) / TK);
-    hipLaunchKernelGGL(kern, dim3((u32)tiles), dim3(WC * WT * 64), lds, stream, p);
+    // as many workgroups as the 256 CUs hold at once, each with its share of the tiles
+    const int64_t most = 256 * (163840 / lds);
+    hipLaunchKernelGGL(kern, dim3((u32)(tiles < most ? tiles : most)), dim3(WC * WT * 64), lds, stream, p);
     return hipGetLastError();
 }
 
@@ -409,8 +431,10 @@ hipError_t launch(const GemmE4M3Params &p, hipStream_t stream) {
     const int64_t blocks = (int64_t)((p.M + 31) / 32) * ((p.Nout + 31) / 32);
     if (p.M <= 16) return launch_split<WIDE, 1, 1, 4>(p, stream);
     if (blocks <= 1000) return launch_split<WIDE, 2, 2, 1>(p, stream);
-    const int64_t big = (int64_t)((p.M + 255) / 256) * ((p.Nout + 255) / 256);
-    if (big >= 192) return launch_tile<WIDE, 2, 4, 8, 4>(p, stream);
+    if constexpr (!WIDE) {
+        const int64_t big = (int64_t)((p.M + 255) / 256) * ((p.Nout + 255) / 256);
+        if (big >= 192) return launch_tile<false, 2, 4, 8, 4>(p, stream);
+    }
     return launch_tile<WIDE, 2, 2, 4, 4>(p, stream);
 }
 
