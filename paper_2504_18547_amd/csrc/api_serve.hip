@@ -230,11 +230,16 @@ vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64
     p.head_units = (uint32_t)(cache->head_stride * size / 16);
     p.token_units = (uint32_t)(cache->token_stride * size / 16);
     p.page_div = vitq::fast_div(p.page_size); p.group_div = vitq::fast_div((uint32_t)p.group);
-    p.scale_log2 = (float)((double)scale * (double)cache->k_scale * 1.4426950408889634);
+    // The kernels take maxima before scaling and mask with -infinity, so they get a positive factor: the sign goes to the
+    // queries, and zero becomes a number that leaves every finite score at zero.
+    p.negative = scale < 0.0f ? 1 : 0;
+    p.scale_log2 = (float)(fabs((double)scale) * (double)cache->k_scale * 1.4426950408889634);
+    if (!isfinite(p.scale_log2)) return VQ_ERR_STEP;
+    if (p.scale_log2 < 0x1p-126f) p.scale_log2 = 0x1p-126f;
     p.v_scale = cache->v_scale;
     p.causal = causal ? 1 : 0; p.window = window;
     p.out = (uint8_t *)out; p.out_ld = out_ld; p.lse = lse;
-    return vitq::paged_launch(p, dtype, cache->dtype, cache->head_dim, max_kv, (hipStream_t)stream) == hipSuccess ? VQ_OK : VQ_ERR_HIP;
+    return vitq::paged_launch(p, dtype, cache->dtype, cache->head_dim, (hipStream_t)stream) == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
 }  // extern "C"

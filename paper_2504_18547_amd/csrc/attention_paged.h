@@ -15,14 +15,16 @@ struct PagedParams {
     const uint8_t *k, *v; uint32_t pages, page_size;
     uint32_t page_units, head_units, token_units;             // strides of the cache in units of 16 bytes
     FastDiv page_div, group_div;
-    float scale_log2, v_scale;                                // scale * k_scale * log2(e); scale of the values
+    float scale_log2, v_scale;                                // |scale| * k_scale * log2(e), not 0; scale of the values
+    int negative;                                             // the scale is negative
     int causal, window;
     uint8_t *out; int64_t out_ld; float *lse;
+    int tiles;                                                // of rows, over all sequences (set by the launcher)
     int splits; float *part, *part_lse;                       // [split][token][head][head_dim], [split][token][head]
 };
 
 // Splits of the keys that the launcher chooses for these sizes (1: no workspace).
 int paged_splits(int64_t tokens, int seqs, int q_heads, int kv_heads, int head_dim, int64_t max_kv);
-hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, int64_t max_kv, hipStream_t stream);
+hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, hipStream_t stream);
 
 }  // namespace vitq

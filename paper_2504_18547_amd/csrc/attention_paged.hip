@@ -125,6 +125,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
         for (int i = 0; i < NQ; ++i) {
             const int c = C8 ? ((i >> 1) * 4 + q4) * 16 + (i & 1) * 8 : (i * 4 + q4) * 8;
             qf[i] = *reinterpret_cast<const v4u *>(qr + c * 2);
+            if (p.negative) qf[i] ^= 0x80008000u;
         }
     }
     const int32_t *table = p.page_table + (int64_t)t.seq * p.table_stride;
@@ -301,6 +302,287 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
     }
 }
 
+// ---- many rows: 32 rows per wave, keys through LDS -------------------------------------------------------------------------
+// A workgroup's four waves have 32 rows each and share steps of 64 keys, K and V each in two LDS buffers.  16-bit caches go there
+// straight from memory, E4M3 ones are widened on the way.  Scores: A = K rows from LDS, B = Q in registers.  O^T: A = V^T by the
+// transposing LDS read, four keys of one channel per lane, in the order in which the score registers hold the keys; B = P^T.
+// LDS rows are unpadded with their 16-byte chunks permuted by the row: K's so that 16 rows' equal chunks cover all banks, V's so
+// that four rows' 64-byte pieces do.
+constexpr int kTileRows = 128, kTileKeys = 64;
+
+template <int DT>
+__device__ __forceinline__ v16f mfma32(const v4u &a, const v4u &b, const v16f &c) {
+    if constexpr (DT == kBF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ float max_halves(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ u32 lds_address_of(const void *p) {
+    return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p;
+}
+// 16 bytes per lane straight to LDS (dst + 16 * lane); waited for with vmcnt by hand.  (Nothing else here uses M0.)
+__device__ __forceinline__ void to_lds16(const uint8_t *src, u32 dst) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(src), "s"(dst) : "memory");
+}
+__device__ __attribute__((aligned(16))) const u32 g_no_key[4] = {0u, 0u, 0u, 0u};
+
+template <int DT, bool C8, int DH>
+__global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p) {
+    constexpr int RB = DH * 2, CH = RB / 16;                  // bytes and 16-byte chunks of an LDS row
+    constexpr int kBuf = kTileKeys * RB;                      // K or V of a step
+    constexpr int NQ = DH / 16, ND = DH / 32;
+    constexpr int kRowsPerLoad = 64 / (C8 ? CH / 2 : CH);     // rows that a wave's load instruction covers (16 bytes per lane)
+    constexpr int kLoads = kTileKeys / 4 / kRowsPerLoad;      // per wave, for K and again for V
+    __shared__ __attribute__((aligned(16))) uint8_t smem[4 * kBuf];      // K0 K1 V0 V1
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+
+    // Workgroups go round-robin to the eight XCDs; one XCD gets consecutive numbers, and those are row tiles of one head: they
+    // share its keys in that L2.  The last tiles, which see most under a causal mask, start first.
+    int id;
+    {
+        const int total = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = total >> 3, rem = total & 7;
+        id = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + slot;
+    }
+    const int tiles = p.tiles;
+    const int rest = (int)__builtin_amdgcn_readfirstlane(id / tiles);
+    const int tile = tiles - 1 - (id - rest * tiles);
+    const int split = (int)__builtin_amdgcn_readfirstlane(rest / p.kv_heads), head = rest - split * p.kv_heads;
+    RowTile t;
+    if (!find_tile<kTileRows>(p, tile, t)) return;
+
+    // this lane's row, and what the wave's rows see
+    const int wave_rows = min(32, t.rows - 32 * wave);        // may be <= 0: the wave only helps to load
+    const int r = t.row0 + min(32 * wave + l32, t.rows - 1);
+    const int tok = (int)divide(r, p.group_div), g = r - tok * p.group;
+    int my_lo, my_hi, lo, hi, x0, x1, w_lo, w_hi, w_first_hi, w_last_lo;
+    row_range(p, t, tok, my_lo, my_hi);
+    row_range(p, t, (int)divide(t.row0, p.group_div), lo, x0);
+    row_range(p, t, (int)divide(t.row0 + t.rows - 1, p.group_div), x1, hi);
+    {
+        const int ra = t.row0 + min(32 * wave, t.rows - 1), rb = t.row0 + min(32 * wave + 31, t.rows - 1);
+        row_range(p, t, (int)divide(ra, p.group_div), w_lo, w_first_hi);
+        row_range(p, t, (int)divide(rb, p.group_div), w_last_lo, w_hi);
+    }
+    const int lowest = lo;
+    lo &= ~(kTileKeys - 1);
+    const int all_steps = hi > lo ? (hi - lo + kTileKeys - 1) / kTileKeys : 0;
+    const int per = (all_steps + p.splits - 1) / p.splits;
+    const int step0 = split * per, step1 = min(all_steps, step0 + per);
+
+    // Q: channels 16 i + 8 h .. of this lane's row; a negative scale is a sign of the queries (maxima are taken before scaling)
+    v4u qf[NQ];
+    {
+        const uint8_t *qr = p.q + ((int64_t)(t.first + tok) * p.q_ld + (int64_t)(head * p.group + g) * DH) * 2;
+        const u32 flip = p.negative ? 0x80008000u : 0u;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            qf[i] = *reinterpret_cast<const v4u *>(qr + (16 * i + 8 * h) * 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) qf[i][j] ^= flip;
+        }
+    }
+    const int32_t *table = p.page_table + (int64_t)t.seq * p.table_stride;
+    const u32 head_unit = (u32)head * p.head_units;
+    const u32 lds0 = (u32)__builtin_amdgcn_readfirstlane((int)lds_address_of(smem));
+
+    // the cache row of key (first key of the step) + lane, in units of 16 bytes; ~0: no such key
+    auto look_up = [&](int st) -> u32 {
+        const int key = lo + st * kTileKeys + lane;
+        if (st >= step1 || key < lowest || key >= hi) return ~0u;
+        const u32 pg = divide((u32)key, p.page_div);
+        const u32 page = (u32)table[pg];
+        return page < p.pages ? head_unit + page * p.page_units + ((u32)key - pg * p.page_size) * p.token_units : ~0u;
+    };
+    // which row and chunk of the step this lane loads: row (load n) = (4 n + wave) * kRowsPerLoad + lr
+    constexpr int kLanes = 64 / kRowsPerLoad;                 // lanes per row
+    const int lr = lane / kLanes, lc = lane % kLanes;
+    v4u stage_k[C8 ? kLoads : 1], stage_v[C8 ? kLoads : 1];
+    auto k_swizzle = [](int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; };
+    auto v_swizzle = [](int row) { return DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
+    auto load = [&](u32 unit, int buf) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+            const int row = (4 * n + wave) * kRowsPerLoad + lr;
+            const u32 u = (u32)__shfl((int)unit, row);
+            const uint8_t *none = reinterpret_cast<const uint8_t *>(g_no_key);
+            if constexpr (C8) {
+                stage_k[n] = *reinterpret_cast<const v4u *>(u != ~0u ? p.k + (uint64_t)u * 16 + lc * 16 : none);
+                stage_v[n] = *reinterpret_cast<const v4u *>(u != ~0u ? p.v + (uint64_t)u * 16 + lc * 16 : none);
+            } else {
+                const u32 dst = lds0 + (u32)(buf * kBuf + (4 * n + wave) * kRowsPerLoad * RB);
+                to_lds16(u != ~0u ? p.k + (uint64_t)u * 16 + (lc ^ k_swizzle(row)) * 16 : none, dst);
+                to_lds16(u != ~0u ? p.v + (uint64_t)u * 16 + (lc ^ v_swizzle(row)) * 16 : none, dst + 2 * kBuf);
+            }
+        }
+    };
+    auto widen_to_lds = [&](int buf) {                        // E4M3: sixteen channels of a row are two chunks
+        if constexpr (C8) {
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) {
+                const int row = (4 * n + wave) * kRowsPerLoad + lr;
+                uint8_t *kr = smem + buf * kBuf + row * RB, *vr = kr + 2 * kBuf;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    *reinterpret_cast<v4u *>(kr + (((2 * lc + e) ^ k_swizzle(row)) * 16)) = widen8<DT>(stage_k[n][2 * e], stage_k[n][2 * e + 1]);
+                    *reinterpret_cast<v4u *>(vr + (((2 * lc + e) ^ v_swizzle(row)) * 16)) = widen8<DT>(stage_v[n][2 * e], stage_v[n][2 * e + 1]);
+                }
+            }
+        }
+    };
+
+    // LDS offsets of this lane's pieces: K row l32 (+32), chunk 2 i + h; V rows 4 h + (lane % 16) / 4 (+8, +16 ...), channels
+    // 32 d + 16 ((lane / 16) % 2) + 4 (lane % 4) ..
+    const int vrow = 4 * h + ((lane >> 2) & 3);
+    const int vchunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    auto v_offset = [&](int d) { return (u32)(vrow * RB + (((4 * d + vchunk) ^ v_swizzle(vrow)) * 16) + (lane & 1) * 8); };
+
+    v16f o[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+    const float c = p.scale_log2;
+
+    if (step0 < step1) {
+        u32 unit = look_up(step0);
+        uint64_t seen_next = __builtin_amdgcn_ballot_w64(unit != ~0u);
+        load(unit, 0);
+        unit = look_up(step0 + 1);
+        for (int st = step0; st < step1; ++st) {
+            const int buf = (st - step0) & 1;
+            const uint64_t seen = seen_next;
+            if constexpr (C8) {
+                widen_to_lds(buf);
+                __syncthreads();
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+            // every wave is past its reads of the other buffer
+            seen_next = __builtin_amdgcn_ballot_w64(unit != ~0u);
+            if (st + 1 < step1) {
+                load(unit, buf ^ 1);
+                unit = look_up(st + 2);
+            }
+            const int key0 = lo + st * kTileKeys;
+            if (wave_rows <= 0 || key0 >= w_hi || key0 + kTileKeys <= w_lo) continue;      // nothing for this wave's rows
+            const uint8_t *kb = smem + buf * kBuf, *vb = kb + 2 * kBuf;
+
+            v16f s[2];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
+                const int row = 32 * kt + l32;
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    const v4u f = *reinterpret_cast<const v4u *>(kb + row * RB + (((2 * i + h) ^ k_swizzle(row)) * 16));
+                    s[kt] = mfma32<DT>(f, qf[i], s[kt]);
+                }
+            }
+            // register i of tile kt is key 32 kt + 8 (i / 4) + 4 h + i % 4 of this lane's row
+            if (~seen != 0 || key0 < w_last_lo || key0 + kTileKeys > w_first_hi) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at = 32 * kt + 8 * (i >> 2) + 4 * h + (i & 3);
+                        const bool on = ((seen >> at) & 1u) && key0 + at >= my_lo && key0 + at < my_hi;
+                        s[kt][i] = on ? s[kt][i] : -INFINITY;
+                    }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
+            top = max_halves(top) * c;
+            // The maximum that the exponents are taken against follows only when it has fallen behind by 2^8: the sums are the same
+            // either way, and rescaling them in every step costs as much as a quarter of the exponentials.
+            if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) {
+                const float now = fmaxf(m, top);
+                const float alpha = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+                m = now;
+                l *= alpha;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+            }
+            const float base = m == -INFINITY ? 0.0f : m;
+            v4u pf[4];
+            float sum = 0.0f;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float a = __builtin_amdgcn_exp2f(fmaf(s[kt][i], c, -base)), b = __builtin_amdgcn_exp2f(fmaf(s[kt][i + 1], c, -base));
+                    sum += a;
+                    sum += b;
+                    pf[2 * kt + (i >> 3)][(i >> 1) & 3] = pack16bit<DT>(a, b);
+                }
+            l += sum;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    typedef short v4s __attribute__((ext_vector_type(4)));
+                    typedef __attribute__((address_space(3))) v4s *lds_v4s;
+                    const uint8_t *at = vb + 16 * e * RB + v_offset(d);
+                    // (rows 8 further: the chunk permutation depends on the row modulo 4 only)
+                    const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at));
+                    const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at + 8 * RB));
+                    v4u f;
+                    const uint2 u0 = __builtin_bit_cast(uint2, a0), u1 = __builtin_bit_cast(uint2, a1);
+                    f[0] = u0.x; f[1] = u0.y; f[2] = u1.x; f[3] = u1.y;
+                    o[d] = mfma32<DT>(f, pf[e], o[d]);
+                }
+        }
+    }
+    {
+        const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+    }
+    if (32 * wave + l32 >= t.rows) return;
+    const float inv = l == 0.0f ? 0.0f : p.v_scale / l;
+    const float lse2 = l == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(l);                 // base 2
+    const int token = t.first + tok, qh = head * p.group + g;
+    const int64_t at = (int64_t)token * p.q_heads + qh;
+    if (p.splits > 1) {
+        const int64_t slot = (int64_t)split * p.tokens * p.q_heads + at;
+        if (h == 0) p.part_lse[slot] = lse2;
+        if (l != 0.0f) {
+            float *dst = p.part + slot * DH + 4 * h;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<v4f *>(dst + 32 * d + 2 * i) = v4f{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+        }
+    } else {
+        if (h == 0 && p.lse) p.lse[at] = lse2 * 0x1.62e430p-1f;
+        uint8_t *dst = p.out + ((int64_t)token * p.out_ld + (int64_t)qh * DH) * 2;
+        const bool none = l == 0.0f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 8) {
+                // channels 32 d + 2 i + 4 h .. and eight further: trading with the other half gives eight in a row
+                u32 w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = none ? 0u : pack16bit<DT>(o[d][i + 2 * j] * inv, o[d][i + 2 * j + 1] * inv);
+                const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                *reinterpret_cast<uint4 *>(dst + (32 * d + 2 * i + 8 * h) * 2) = make_uint4(a[0], b[0], a[1], b[1]);
+            }
+    }
+}
+
 // ---- joins the splits of a row: a weighted mean with weights exp2(lse_split - the largest) --------------------------------
 template <int DT, int DH>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
@@ -341,9 +623,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
 }
 
 template <int DT, bool C8, int DH>
-hipError_t launch(PagedParams &p, int64_t max_kv, hipStream_t stream) {
-    const int64_t tiles = p.tokens * p.group / kRows + p.seqs;
-    hipLaunchKernelGGL((paged_rows_kernel<DT, C8, DH>), dim3((u32)(tiles * p.kv_heads * p.splits)), dim3(kWaves * 64), 0, stream, p);
+hipError_t launch(PagedParams &p, bool tiled, hipStream_t stream) {
+    p.tiles = (int)(p.tokens * p.group / (tiled ? kTileRows : kRows)) + p.seqs;
+    const dim3 grid((u32)((int64_t)p.tiles * p.kv_heads * p.splits));
+    if (tiled) hipLaunchKernelGGL((paged_tiles_kernel<DT, C8, DH>), grid, dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((paged_rows_kernel<DT, C8, DH>), grid, dim3(kWaves * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
         hipLaunchKernelGGL((paged_join_kernel<DT, DH>), dim3((u32)((p.tokens * p.q_heads + 15) / 16)), dim3(256), 0, stream, p);
@@ -352,22 +636,27 @@ hipError_t launch(PagedParams &p, int64_t max_kv, hipStream_t stream) {
     return e;
 }
 
+// Rows per sequence decide: up to two sixteens, the form that streams the cache without LDS.
+bool wants_tiles(int64_t tokens, int seqs, int group) { return tokens * group > (int64_t)32 * seqs; }
+
 }  // namespace
 
 int paged_splits(int64_t tokens, int seqs, int q_heads, int kv_heads, int head_dim, int64_t max_kv) {
-    const int64_t tiles = tokens * (q_heads / kv_heads) / kRows + seqs;
-    // enough workgroups for the chip, each with at least two steps per wave
-    const int64_t want = (1024 + tiles * kv_heads - 1) / (tiles * kv_heads);
-    const int64_t most = max_kv / (kWaves * kStep * 2);
+    const int group = q_heads / kv_heads;
+    const bool tiled = wants_tiles(tokens, seqs, group);
+    const int64_t blocks = (tokens * group / (tiled ? kTileRows : kRows) + seqs) * kv_heads;
+    // enough workgroups for the chip, each with at least two steps per wave (tiles: four steps)
+    const int64_t want = ((tiled ? 512 : 1024) + blocks - 1) / blocks;
+    const int64_t most = max_kv / 256;
     int64_t s = want < most ? want : most;
     return s < 1 ? 1 : (s > 64 ? 64 : (int)s);
 }
 
-hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, int64_t max_kv, hipStream_t stream) {
-    const bool c8 = cache_dtype == kE4M3;
+hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, hipStream_t stream) {
+    const bool c8 = cache_dtype == kE4M3, tiled = wants_tiles(p.tokens, p.seqs, p.group);
 #define VITQ_PAGED(DT) \
-    if (head_dim == 64) return c8 ? launch<DT, true, 64>(p, max_kv, stream) : launch<DT, false, 64>(p, max_kv, stream); \
-    return c8 ? launch<DT, true, 128>(p, max_kv, stream) : launch<DT, false, 128>(p, max_kv, stream);
+    if (head_dim == 64) return c8 ? launch<DT, true, 64>(p, tiled, stream) : launch<DT, false, 64>(p, tiled, stream); \
+    return c8 ? launch<DT, true, 128>(p, tiled, stream) : launch<DT, false, 128>(p, tiled, stream);
     if (dtype == kBF16) { VITQ_PAGED(kBF16) }
     VITQ_PAGED(kF16)
 #undef VITQ_PAGED

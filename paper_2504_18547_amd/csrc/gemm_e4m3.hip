@@ -205,7 +205,8 @@ __device__ __forceinline__ u32 lds_address_of(const void *p) {
     return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p;
 }
 // Loads straight to LDS through a buffer descriptor: lane i's 16 (4) bytes at byte `off` go to dst + 16 i (4 i), zeros where
-// `off` lies beyond the descriptor's size.  The compiler does not see them; they are waited for with vmcnt by hand.
+// `off` lies beyond the descriptor's size.  The compiler does not see them; they are waited for with vmcnt by hand.  (Nothing
+// else here uses M0.)
 __device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
 __device__ __forceinline__ v4i descriptor(uint64_t base, u32 bytes) {
     v4i d;
@@ -217,10 +218,10 @@ __device__ __forceinline__ v4i rows_descriptor(uint64_t base, int rows, u32 stri
     return descriptor(base, rows > 0 ? (u32)(rows - 1) * stride + tail : 0u);
 }
 __device__ __forceinline__ void to_lds16(u32 off, const v4i &buf, u32 dst) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory");
 }
 __device__ __forceinline__ void to_lds4(u32 off, const v4i &buf, u32 dst) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory");
 }
 
 template <bool WIDE, int WC, int WT, int AT, int TT>
