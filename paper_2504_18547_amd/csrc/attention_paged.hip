@@ -367,6 +367,7 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
         row_range(p, t, (int)divide(ra, p.group_div), w_lo, w_first_hi);
         row_range(p, t, (int)divide(rb, p.group_div), w_last_lo, w_hi);
     }
+    const u32 my_span = (u32)(my_hi - my_lo);
     const int lowest = lo;
     lo &= ~(kTileKeys - 1);
     const int all_steps = hi > lo ? (hi - lo + kTileKeys - 1) / kTileKeys : 0;
@@ -389,46 +390,54 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
     const u32 head_unit = (u32)head * p.head_units;
     const u32 lds0 = (u32)__builtin_amdgcn_readfirstlane((int)lds_address_of(smem));
 
-    // the cache row of key (first key of the step) + lane, in units of 16 bytes; ~0: no such key
-    auto look_up = [&](int st) -> u32 {
+    // The cache row of key (first key of the step) + lane, in units of 16 bytes, ~0 where there is none.  Its page number is
+    // requested a step before it is looked at: between the two all loads are waited for anyway.
+    u32 asked_page = ~0u, asked_place = 0;
+    auto ask = [&](int st) {
         const int key = lo + st * kTileKeys + lane;
-        if (st >= step1 || key < lowest || key >= hi) return ~0u;
-        const u32 pg = divide((u32)key, p.page_div);
-        const u32 page = (u32)table[pg];
-        return page < p.pages ? head_unit + page * p.page_units + ((u32)key - pg * p.page_size) * p.token_units : ~0u;
+        const bool want = st < step1 && key >= lowest && key < hi;
+        const u32 pg = divide((u32)(want ? key : lowest), p.page_div);
+        asked_page = (u32)table[pg];                          // (some page of this sequence where the lane has no key)
+        asked_place = want ? (u32)key - pg * p.page_size : ~0u;
     };
-    // which row and chunk of the step this lane loads: row (load n) = (4 n + wave) * kRowsPerLoad + lr
-    constexpr int kLanes = 64 / kRowsPerLoad;                 // lanes per row
-    const int lr = lane / kLanes, lc = lane % kLanes;
+    auto answer = [&]() -> u32 {
+        return asked_place != ~0u && asked_page < p.pages ? head_unit + asked_page * p.page_units + asked_place * p.token_units : ~0u;
+    };
+    // Which row and chunk of the step this lane loads: row0 + kNext n for load n.  kNext is a multiple of what the permutations of
+    // the chunks look at, so they are the same for every n.
+    constexpr int kLanes = 64 / kRowsPerLoad, kNext = 4 * kRowsPerLoad;
+    const int row0 = wave * kRowsPerLoad + lane / kLanes, lc = lane % kLanes;
     v4u stage_k[C8 ? kLoads : 1], stage_v[C8 ? kLoads : 1];
     auto k_swizzle = [](int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; };
     auto v_swizzle = [](int row) { return DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
+    const uint8_t *k_lane = p.k + (C8 ? lc : lc ^ k_swizzle(row0)) * 16, *v_lane = p.v + (C8 ? lc : lc ^ v_swizzle(row0)) * 16;
     auto load = [&](u32 unit, int buf) {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-            const int row = (4 * n + wave) * kRowsPerLoad + lr;
-            const u32 u = (u32)__shfl((int)unit, row);
+            const u32 u = (u32)__builtin_amdgcn_ds_bpermute(4 * row0 + 4 * kNext * n, (int)unit);
+            const uint64_t at = (uint64_t)u * 16;
             const uint8_t *none = reinterpret_cast<const uint8_t *>(g_no_key);
+            const uint8_t *ks = u != ~0u ? k_lane + at : none, *vs = u != ~0u ? v_lane + at : none;
             if constexpr (C8) {
-                stage_k[n] = *reinterpret_cast<const v4u *>(u != ~0u ? p.k + (uint64_t)u * 16 + lc * 16 : none);
-                stage_v[n] = *reinterpret_cast<const v4u *>(u != ~0u ? p.v + (uint64_t)u * 16 + lc * 16 : none);
+                stage_k[n] = *reinterpret_cast<const v4u *>(ks);
+                stage_v[n] = *reinterpret_cast<const v4u *>(vs);
             } else {
                 const u32 dst = lds0 + (u32)(buf * kBuf + (4 * n + wave) * kRowsPerLoad * RB);
-                to_lds16(u != ~0u ? p.k + (uint64_t)u * 16 + (lc ^ k_swizzle(row)) * 16 : none, dst);
-                to_lds16(u != ~0u ? p.v + (uint64_t)u * 16 + (lc ^ v_swizzle(row)) * 16 : none, dst + 2 * kBuf);
+                to_lds16(ks, dst);
+                to_lds16(vs, dst + 2 * kBuf);
             }
         }
     };
     auto widen_to_lds = [&](int buf) {                        // E4M3: sixteen channels of a row are two chunks
         if constexpr (C8) {
+            uint8_t *kr = smem + buf * kBuf + row0 * RB, *vr = kr + 2 * kBuf;
+            const int kc = ((2 * lc) ^ k_swizzle(row0)) * 16, vc = ((2 * lc) ^ v_swizzle(row0)) * 16;
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
-                const int row = (4 * n + wave) * kRowsPerLoad + lr;
-                uint8_t *kr = smem + buf * kBuf + row * RB, *vr = kr + 2 * kBuf;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    *reinterpret_cast<v4u *>(kr + (((2 * lc + e) ^ k_swizzle(row)) * 16)) = widen8<DT>(stage_k[n][2 * e], stage_k[n][2 * e + 1]);
-                    *reinterpret_cast<v4u *>(vr + (((2 * lc + e) ^ v_swizzle(row)) * 16)) = widen8<DT>(stage_v[n][2 * e], stage_v[n][2 * e + 1]);
+                    *reinterpret_cast<v4u *>(kr + kNext * n * RB + (kc ^ (16 * e))) = widen8<DT>(stage_k[n][2 * e], stage_k[n][2 * e + 1]);
+                    *reinterpret_cast<v4u *>(vr + kNext * n * RB + (vc ^ (16 * e))) = widen8<DT>(stage_v[n][2 * e], stage_v[n][2 * e + 1]);
                 }
             }
         }
@@ -449,10 +458,11 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
     const float c = p.scale_log2;
 
     if (step0 < step1) {
-        u32 unit = look_up(step0);
+        ask(step0);
+        u32 unit = answer();
         uint64_t seen_next = __builtin_amdgcn_ballot_w64(unit != ~0u);
+        ask(step0 + 1);
         load(unit, 0);
-        unit = look_up(step0 + 1);
         for (int st = step0; st < step1; ++st) {
             const int buf = (st - step0) & 1;
             const uint64_t seen = seen_next;
@@ -465,27 +475,45 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
                 asm volatile("" ::: "memory");
             }
             // every wave is past its reads of the other buffer
+            unit = answer();
             seen_next = __builtin_amdgcn_ballot_w64(unit != ~0u);
-            if (st + 1 < step1) {
-                load(unit, buf ^ 1);
-                unit = look_up(st + 2);
-            }
+            ask(st + 2);
+            if (st + 1 < step1) load(unit, buf ^ 1);
             const int key0 = lo + st * kTileKeys;
             if (wave_rows <= 0 || key0 >= w_hi || key0 + kTileKeys <= w_lo) continue;      // nothing for this wave's rows
             const uint8_t *kb = smem + buf * kBuf, *vb = kb + 2 * kBuf;
 
+            // Scores: the two key tiles in turn, so that no product waits for the one before it, operands read kAhead products ahead.
+            constexpr int kAhead = 4;
             v16f s[2];
+            v4u kf[kAhead];
+            auto k_read = [&](int n) {
+                const int row = 32 * (n & 1) + l32;
+                return *reinterpret_cast<const v4u *>(kb + row * RB + (((2 * (n >> 1) + h) ^ k_swizzle(row)) * 16));
+            };
+            static_for<kAhead>([&](auto N) { kf[decltype(N)::value] = k_read(decltype(N)::value); });
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
-                const int row = 32 * kt + l32;
-#pragma unroll
-                for (int i = 0; i < NQ; ++i) {
-                    const v4u f = *reinterpret_cast<const v4u *>(kb + row * RB + (((2 * i + h) ^ k_swizzle(row)) * 16));
-                    s[kt] = mfma32<DT>(f, qf[i], s[kt]);
-                }
-            }
+            for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
+            static_for<2 * NQ>([&](auto N) {
+                constexpr int n = decltype(N)::value;
+                s[n & 1] = mfma32<DT>(kf[n % kAhead], qf[n >> 1], s[n & 1]);
+                if constexpr (n + kAhead < 2 * NQ) kf[n % kAhead] = k_read(n + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            // The first V operands are on their way while the softmax runs.  Operand n: keys 16 (n / ND) .., channels 32 (n % ND) ..
+            v4u vf[kAhead];
+            auto v_read = [&](int n) {
+                typedef short v4s __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) v4s *lds_v4s;
+                const uint8_t *at = vb + 16 * (n / ND) * RB + v_offset(n % ND);
+                // (rows 8 further: the chunk permutation depends on the row modulo 4 only)
+                const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at));
+                const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at + 8 * RB));
+                const uint2 u0 = __builtin_bit_cast(uint2, a0), u1 = __builtin_bit_cast(uint2, a1);
+                return v4u{u0.x, u0.y, u1.x, u1.y};
+            };
+            static_for<kAhead>([&](auto N) { vf[decltype(N)::value] = v_read(decltype(N)::value); });
+            __builtin_amdgcn_sched_barrier(0);
             // register i of tile kt is key 32 kt + 8 (i / 4) + 4 h + i % 4 of this lane's row
             if (~seen != 0 || key0 < w_last_lo || key0 + kTileKeys > w_first_hi) {
 #pragma unroll
@@ -493,10 +521,11 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int at = 32 * kt + 8 * (i >> 2) + 4 * h + (i & 3);
-                        const bool on = ((seen >> at) & 1u) && key0 + at >= my_lo && key0 + at < my_hi;
+                        const bool on = ((seen >> at) & 1u) && (u32)(key0 + at - my_lo) < my_span;
                         s[kt][i] = on ? s[kt][i] : -INFINITY;
                     }
             }
+            asm volatile("" : "+v"(s[0]), "+v"(s[1]));        // both ways end in the same registers
             float top = s[0][0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
@@ -516,33 +545,31 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
                     for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
             }
             const float base = m == -INFINITY ? 0.0f : m;
-            v4u pf[4];
-            float sum = 0.0f;
+            // Probabilities 2 w, 2 w + 1 of the sixteen keys of group e.  Those of the next group are computed between the products
+            // of this one.
+            v4u pf[2];
+            float sum[2] = {0.0f, 0.0f};
+            auto exps = [&](int e, int w) {
+                const float a = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][8 * (e & 1) + 2 * w], c, -base));
+                const float b = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][8 * (e & 1) + 2 * w + 1], c, -base));
+                sum[0] += a;
+                sum[1] += b;
+                pf[e & 1][w] = pack16bit<DT>(a, b);
+            };
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int w = 0; w < 4; ++w) exps(0, w);
+            __builtin_amdgcn_sched_barrier(0);
+            static_for<4 * ND>([&](auto N) {
+                constexpr int n = decltype(N)::value, e = n / ND, d = n % ND;
+                o[d] = mfma32<DT>(vf[n % kAhead], pf[e & 1], o[d]);
+                if constexpr (n + kAhead < 4 * ND) vf[n % kAhead] = v_read(n + kAhead);
+                if constexpr (e < 3) {
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float a = __builtin_amdgcn_exp2f(fmaf(s[kt][i], c, -base)), b = __builtin_amdgcn_exp2f(fmaf(s[kt][i + 1], c, -base));
-                    sum += a;
-                    sum += b;
-                    pf[2 * kt + (i >> 3)][(i >> 1) & 3] = pack16bit<DT>(a, b);
+                    for (int w = 4 / ND * d; w < 4 / ND * (d + 1); ++w) exps(e + 1, w);
                 }
-            l += sum;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    typedef short v4s __attribute__((ext_vector_type(4)));
-                    typedef __attribute__((address_space(3))) v4s *lds_v4s;
-                    const uint8_t *at = vb + 16 * e * RB + v_offset(d);
-                    // (rows 8 further: the chunk permutation depends on the row modulo 4 only)
-                    const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at));
-                    const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at + 8 * RB));
-                    v4u f;
-                    const uint2 u0 = __builtin_bit_cast(uint2, a0), u1 = __builtin_bit_cast(uint2, a1);
-                    f[0] = u0.x; f[1] = u0.y; f[2] = u1.x; f[3] = u1.y;
-                    o[d] = mfma32<DT>(f, pf[e], o[d]);
-                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            l += sum[0] + sum[1];
         }
     }
     {
