@@ -229,6 +229,7 @@ vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64
     p.page_units = (uint32_t)(cache->page_stride * size / 16);
     p.head_units = (uint32_t)(cache->head_stride * size / 16);
     p.token_units = (uint32_t)(cache->token_stride * size / 16);
+    p.whole_rows = p.page_size % 16 == 0 && p.token_units < (1u << 23);
     p.page_div = vitq::fast_div(p.page_size); p.group_div = vitq::fast_div((uint32_t)p.group);
     // The kernels take maxima before scaling and mask with -infinity, so they get a positive factor: the sign goes to the
     // queries, and zero becomes a number that leaves every finite score at zero.

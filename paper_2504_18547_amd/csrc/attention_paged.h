@@ -14,6 +14,7 @@ struct PagedParams {
     const int32_t *page_table; int64_t table_stride; int table_cols;
     const uint8_t *k, *v; uint32_t pages, page_size;
     uint32_t page_units, head_units, token_units;             // strides of the cache in units of 16 bytes
+    int whole_rows;                                           // sixteen aligned keys lie in one page, within 2^31 bytes
     FastDiv page_div, group_div;
     float scale_log2, v_scale;                                // |scale| * k_scale * log2(e), not 0; scale of the values
     int negative;                                             // the scale is negative

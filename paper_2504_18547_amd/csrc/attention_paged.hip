@@ -308,7 +308,6 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
 // transposing LDS read, four keys of one channel per lane, in the order in which the score registers hold the keys; B = P^T.
 // LDS rows are unpadded with their 16-byte chunks permuted by the row: K's so that 16 rows' equal chunks cover all banks, V's so
 // that four rows' 64-byte pieces do.
-constexpr int kTileRows = 128, kTileKeys = 64;
 
 template <int DT>
 __device__ __forceinline__ v16f mfma32(const v4u &a, const v4u &b, const v16f &c) {
@@ -323,18 +322,25 @@ __device__ __forceinline__ u32 lds_address_of(const void *p) {
     return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p;
 }
 // 16 bytes per lane straight to LDS (dst + 16 * lane); waited for with vmcnt by hand.  (Nothing else here uses M0.)
-__device__ __forceinline__ void to_lds16(const uint8_t *src, u32 dst) {
+__device__ __forceinline__ void to_lds16(u32 off, const uint8_t *base, u32 dst) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(base), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void to_lds16_ptr(const uint8_t *src, u32 dst) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(src), "s"(dst) : "memory");
 }
 __device__ __attribute__((aligned(16))) const u32 g_no_key[4] = {0u, 0u, 0u, 0u};
 
-template <int DT, bool C8, int DH>
-__global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p) {
-    constexpr int RB = DH * 2, CH = RB / 16;                  // bytes and 16-byte chunks of an LDS row
+template <int DT, bool C8, int DH, int W>
+__global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParams p) {
+    constexpr int kTileKeys = 64;
+    constexpr int RB = DH * 2;                                // bytes of an LDS row
     constexpr int kBuf = kTileKeys * RB;                      // K or V of a step
     constexpr int NQ = DH / 16, ND = DH / 32;
-    constexpr int kRowsPerLoad = 64 / (C8 ? CH / 2 : CH);     // rows that a wave's load instruction covers (16 bytes per lane)
-    constexpr int kLoads = kTileKeys / 4 / kRowsPerLoad;      // per wave, for K and again for V
+    constexpr int kBytes = C8 && DH == 64 ? 8 : 16;           // that a lane loads at a time
+    constexpr int kRowsPerLoad = 64 * kBytes / (C8 ? DH : RB);      // rows that a wave's load instruction covers
+    constexpr int kLoads = kTileKeys / W / kRowsPerLoad;      // per wave, for K and again for V
+    constexpr int kTileRows = 32 * W;
+    static_assert(kLoads > 0 && kRowsPerLoad <= 16, "every wave loads whole rows");
     __shared__ __attribute__((aligned(16))) uint8_t smem[4 * kBuf];      // K0 K1 V0 V1
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -405,43 +411,54 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
     };
     // Which row and chunk of the step this lane loads: row0 + kNext n for load n.  kNext is a multiple of what the permutations of
     // the chunks look at, so they are the same for every n.
-    constexpr int kLanes = 64 / kRowsPerLoad, kNext = 4 * kRowsPerLoad;
+    constexpr int kLanes = 64 / kRowsPerLoad, kNext = W * kRowsPerLoad;
     const int row0 = wave * kRowsPerLoad + lane / kLanes, lc = lane % kLanes;
-    v4u stage_k[C8 ? kLoads : 1], stage_v[C8 ? kLoads : 1];
+    typedef u32 Stage __attribute__((ext_vector_type(kBytes / 4)));
+    Stage stage_k[C8 ? kLoads : 1], stage_v[C8 ? kLoads : 1];
     auto k_swizzle = [](int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; };
     auto v_swizzle = [](int row) { return DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
-    const uint8_t *k_lane = p.k + (C8 ? lc : lc ^ k_swizzle(row0)) * 16, *v_lane = p.v + (C8 ? lc : lc ^ v_swizzle(row0)) * 16;
-    auto load = [&](u32 unit, int buf) {
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            const u32 u = (u32)__builtin_amdgcn_ds_bpermute(4 * row0 + 4 * kNext * n, (int)unit);
-            const uint64_t at = (uint64_t)u * 16;
-            const uint8_t *none = reinterpret_cast<const uint8_t *>(g_no_key);
-            const uint8_t *ks = u != ~0u ? k_lane + at : none, *vs = u != ~0u ? v_lane + at : none;
-            if constexpr (C8) {
-                stage_k[n] = *reinterpret_cast<const v4u *>(ks);
-                stage_v[n] = *reinterpret_cast<const v4u *>(vs);
-            } else {
-                const u32 dst = lds0 + (u32)(buf * kBuf + (4 * n + wave) * kRowsPerLoad * RB);
-                to_lds16(ks, dst);
-                to_lds16(vs, dst + 2 * kBuf);
-            }
-        }
-    };
-    auto widen_to_lds = [&](int buf) {                        // E4M3: sixteen channels of a row are two chunks
-        if constexpr (C8) {
-            uint8_t *kr = smem + buf * kBuf + row0 * RB, *vr = kr + 2 * kBuf;
-            const int kc = ((2 * lc) ^ k_swizzle(row0)) * 16, vc = ((2 * lc) ^ v_swizzle(row0)) * 16;
+    // The rows of a load instruction lie in one page wherever pages are multiples of sixteen tokens: then their place is a scalar
+    // and a constant per lane.  A step with keys that do not exist, or other page sizes: one address per lane, zeros for no key.
+    const u32 k_lane = (u32)(lane / kLanes) * p.token_units * 16u + (u32)(C8 ? lc : lc ^ k_swizzle(row0)) * kBytes;
+    const u32 v_lane = (u32)(lane / kLanes) * p.token_units * 16u + (u32)(C8 ? lc : lc ^ v_swizzle(row0)) * kBytes;
+    // (rows of a step, `all`: none is missing, into buffer `buf`; E4M3 into registers first)
+    auto load = [&](u32 unit, bool all, int buf, auto IsV) {
+        constexpr bool is_v = decltype(IsV)::value;
+        const u32 dst0 = lds0 + (u32)((is_v ? 2 * kBuf : 0) + buf * kBuf + wave * kRowsPerLoad * RB);
+        const uint8_t *cache = is_v ? p.v : p.k;
+        const u32 in_lane = is_v ? v_lane : k_lane;
+        if (all && p.whole_rows) {
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
+                const uint8_t *row = cache + (uint64_t)(u32)__builtin_amdgcn_readlane((int)unit, wave * kRowsPerLoad + kNext * n) * 16;
+                if constexpr (C8) (is_v ? stage_v : stage_k)[n] = *reinterpret_cast<const Stage *>(row + in_lane);
+                else to_lds16(in_lane, row, dst0 + n * (kNext * RB));
+            }
+        } else {
+            const u32 in_row = in_lane - (u32)(lane / kLanes) * p.token_units * 16u;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    *reinterpret_cast<v4u *>(kr + kNext * n * RB + (kc ^ (16 * e))) = widen8<DT>(stage_k[n][2 * e], stage_k[n][2 * e + 1]);
-                    *reinterpret_cast<v4u *>(vr + kNext * n * RB + (vc ^ (16 * e))) = widen8<DT>(stage_v[n][2 * e], stage_v[n][2 * e + 1]);
-                }
+            for (int n = 0; n < kLoads; ++n) {
+                const u32 u = (u32)__builtin_amdgcn_ds_bpermute(4 * row0 + 4 * kNext * n, (int)unit);
+                const uint8_t *src = u != ~0u ? cache + (uint64_t)u * 16 + in_row : reinterpret_cast<const uint8_t *>(g_no_key);
+                if constexpr (C8) (is_v ? stage_v : stage_k)[n] = *reinterpret_cast<const Stage *>(src);
+                else to_lds16_ptr(src, dst0 + n * (kNext * RB));
             }
         }
     };
+    auto widen_to_lds = [&](int buf, auto IsV) {              // E4M3: eight channels are a chunk
+        constexpr bool is_v = decltype(IsV)::value;
+        constexpr int chunks = kBytes / 8;
+        uint8_t *row = smem + (is_v ? 2 * kBuf : 0) + buf * kBuf + row0 * RB;
+        const int chunk = ((chunks * lc) ^ (is_v ? v_swizzle(row0) : k_swizzle(row0))) * 16;
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+            const Stage &w = (is_v ? stage_v : stage_k)[n];
+#pragma unroll
+            for (int e = 0; e < chunks; ++e) *reinterpret_cast<v4u *>(row + kNext * n * RB + (chunk ^ (16 * e))) = widen8<DT>(w[2 * e], w[2 * e + 1]);
+        }
+    };
+    const std::integral_constant<bool, false> K;
+    const std::integral_constant<bool, true> V;
 
     // LDS offsets of this lane's pieces: K row l32 (+32), chunk 2 i + h; V rows 4 h + (lane % 16) / 4 (+8, +16 ...), channels
     // 32 d + 16 ((lane / 16) % 2) + 4 (lane % 4) ..
@@ -449,127 +466,190 @@ __global__ __launch_bounds__(256, 2) void paged_tiles_kernel(const PagedParams p
     const int vchunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
     auto v_offset = [&](int d) { return (u32)(vrow * RB + (((4 * d + vchunk) ^ v_swizzle(vrow)) * 16) + (lane & 1) * 8); };
 
-    v16f o[ND];
+    v16f o[ND], s[2];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
     const float c = p.scale_log2;
+    v4u pf[4];                                                // probabilities: group e is keys 16 e .. of the step
 
-    if (step0 < step1) {
-        ask(step0);
-        u32 unit = answer();
-        uint64_t seen_next = __builtin_amdgcn_ballot_w64(unit != ~0u);
-        ask(step0 + 1);
-        load(unit, 0);
-        for (int st = step0; st < step1; ++st) {
-            const int buf = (st - step0) & 1;
-            const uint64_t seen = seen_next;
-            if constexpr (C8) {
-                widen_to_lds(buf);
-                __syncthreads();
-            } else {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-            }
-            // every wave is past its reads of the other buffer
-            unit = answer();
-            seen_next = __builtin_amdgcn_ballot_w64(unit != ~0u);
-            ask(st + 2);
-            if (st + 1 < step1) load(unit, buf ^ 1);
-            const int key0 = lo + st * kTileKeys;
-            if (wave_rows <= 0 || key0 >= w_hi || key0 + kTileKeys <= w_lo) continue;      // nothing for this wave's rows
-            const uint8_t *kb = smem + buf * kBuf, *vb = kb + 2 * kBuf;
-
-            // Scores: the two key tiles in turn, so that no product waits for the one before it, operands read kAhead products ahead.
-            constexpr int kAhead = 4;
-            v16f s[2];
-            v4u kf[kAhead];
-            auto k_read = [&](int n) {
-                const int row = 32 * (n & 1) + l32;
-                return *reinterpret_cast<const v4u *>(kb + row * RB + (((2 * (n >> 1) + h) ^ k_swizzle(row)) * 16));
-            };
-            static_for<kAhead>([&](auto N) { kf[decltype(N)::value] = k_read(decltype(N)::value); });
+    // Products with the operands read kAhead ahead.  Product n of the output: keys 16 (n / ND) .., channels 32 (n % ND) ..; product
+    // n of the scores: key tile n % 2, channels 16 (n / 2) ..
+    constexpr int kAhead = 4, kOut = 4 * ND, kScore = 2 * NQ;
+    auto v_read = [&](const uint8_t *vb, int n) {
+        typedef short v4s __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) v4s *lds_v4s;
+        const uint8_t *at = vb + 16 * (n / ND) * RB + v_offset(n % ND);
+        // (rows 8 further: the chunk permutation depends on the row modulo 4 only)
+        const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at));
+        const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at + 8 * RB));
+        const uint2 u0 = __builtin_bit_cast(uint2, a0), u1 = __builtin_bit_cast(uint2, a1);
+        return v4u{u0.x, u0.y, u1.x, u1.y};
+    };
+    auto k_read = [&](const uint8_t *kb, int n) {
+        const int row = 32 * (n & 1) + l32;
+        return *reinterpret_cast<const v4u *>(kb + row * RB + (((2 * (n >> 1) + h) ^ k_swizzle(row)) * 16));
+    };
+    // the products of a step: the output of the step before (OUT), then the scores of this one (SCORE)
+    auto products = [&](auto Out, auto Score, const uint8_t *vb, const uint8_t *kb) {
+        constexpr int outs = decltype(Out)::value ? kOut : 0, all = outs + (decltype(Score)::value ? kScore : 0);
+        v4u f[kAhead];
+        auto read = [&](auto N) {
+            constexpr int n = decltype(N)::value;
+            if constexpr (n < outs) f[n % kAhead] = v_read(vb, n);
+            else f[n % kAhead] = k_read(kb, n - outs);
+        };
+        static_for<kAhead>(read);
+        __builtin_amdgcn_s_setprio(1);                        // ahead of the other group's softmax
+        if constexpr (decltype(Score)::value) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.0f;
-            static_for<2 * NQ>([&](auto N) {
-                constexpr int n = decltype(N)::value;
-                s[n & 1] = mfma32<DT>(kf[n % kAhead], qf[n >> 1], s[n & 1]);
-                if constexpr (n + kAhead < 2 * NQ) kf[n % kAhead] = k_read(n + kAhead);
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            // The first V operands are on their way while the softmax runs.  Operand n: keys 16 (n / ND) .., channels 32 (n % ND) ..
-            v4u vf[kAhead];
-            auto v_read = [&](int n) {
-                typedef short v4s __attribute__((ext_vector_type(4)));
-                typedef __attribute__((address_space(3))) v4s *lds_v4s;
-                const uint8_t *at = vb + 16 * (n / ND) * RB + v_offset(n % ND);
-                // (rows 8 further: the chunk permutation depends on the row modulo 4 only)
-                const v4s a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at));
-                const v4s a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(uintptr_t)lds_address_of(at + 8 * RB));
-                const uint2 u0 = __builtin_bit_cast(uint2, a0), u1 = __builtin_bit_cast(uint2, a1);
-                return v4u{u0.x, u0.y, u1.x, u1.y};
-            };
-            static_for<kAhead>([&](auto N) { vf[decltype(N)::value] = v_read(decltype(N)::value); });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<all>([&](auto N) {
+            constexpr int n = decltype(N)::value;
+            if constexpr (n < outs) o[n % ND] = mfma32<DT>(f[n % kAhead], pf[n / ND], o[n % ND]);
+            else s[(n - outs) & 1] = mfma32<DT>(f[n % kAhead], qf[(n - outs) >> 1], s[(n - outs) & 1]);
+            if constexpr (n + kAhead < all) read(std::integral_constant<int, n + kAhead>{});
             __builtin_amdgcn_sched_barrier(0);
-            // register i of tile kt is key 32 kt + 8 (i / 4) + 4 h + i % 4 of this lane's row
-            if (~seen != 0 || key0 < w_last_lo || key0 + kTileKeys > w_first_hi) {
+        });
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // from the scores of step `st` to its probabilities.  Register i of tile kt is key 32 kt + 8 (i / 4) + 4 h + i % 4.
+    auto softmax = [&](int st, uint64_t seen) {
+        const int key0 = lo + st * kTileKeys;
+        if (~seen != 0 || key0 < w_last_lo || key0 + kTileKeys > w_first_hi) {
+            const int first = key0 + 4 * h - my_lo;               // this lane's key 0 against what its row sees
+            const uint64_t mine = seen >> (4 * h);
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < 2; ++kt) {
+                const u32 there = (u32)(mine >> (32 * kt));
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int at = 32 * kt + 8 * (i >> 2) + 4 * h + (i & 3);
-                        const bool on = ((seen >> at) & 1u) && (u32)(key0 + at - my_lo) < my_span;
-                        s[kt][i] = on ? s[kt][i] : -INFINITY;
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const int at = 8 * (i >> 2) + (i & 3);
+                    const bool on = (there & (1u << at)) != 0 && (u32)(first + 32 * kt + at) < my_span;
+                    s[kt][i] = on ? s[kt][i] : -INFINITY;
+                }
             }
-            asm volatile("" : "+v"(s[0]), "+v"(s[1]));        // both ways end in the same registers
-            float top = s[0][0];
+        }
+        asm volatile("" : "+v"(s[0]), "+v"(s[1]));            // both ways end in the same registers
+        float top = s[0][0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
-            top = max_halves(top) * c;
-            // The maximum that the exponents are taken against follows only when it has fallen behind by 2^8: the sums are the same
-            // either way, and rescaling them in every step costs as much as a quarter of the exponentials.
-            if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) {
-                const float now = fmaxf(m, top);
-                const float alpha = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
-                m = now;
-                l *= alpha;
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
+        top = max_halves(top) * c;
+        // The maximum that the exponents are taken against follows only when it has fallen behind by 2^8: the sums are the same
+        // either way, and rescaling them in every step costs as much as a quarter of the exponentials.
+        if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) {
+            const float now = fmaxf(m, top);
+            const float alpha = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
+            m = now;
+            l *= alpha;
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-            }
-            const float base = m == -INFINITY ? 0.0f : m;
-            // Probabilities 2 w, 2 w + 1 of the sixteen keys of group e.  Those of the next group are computed between the products
-            // of this one.
-            v4u pf[2];
-            float sum[2] = {0.0f, 0.0f};
-            auto exps = [&](int e, int w) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][8 * (e & 1) + 2 * w], c, -base));
-                const float b = __builtin_amdgcn_exp2f(fmaf(s[e >> 1][8 * (e & 1) + 2 * w + 1], c, -base));
+                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = __builtin_amdgcn_exp2f(fmaf(s[kt][i], c, -base)), b = __builtin_amdgcn_exp2f(fmaf(s[kt][i + 1], c, -base));
                 sum[0] += a;
                 sum[1] += b;
-                pf[e & 1][w] = pack16bit<DT>(a, b);
-            };
-#pragma unroll
-            for (int w = 0; w < 4; ++w) exps(0, w);
-            __builtin_amdgcn_sched_barrier(0);
-            static_for<4 * ND>([&](auto N) {
-                constexpr int n = decltype(N)::value, e = n / ND, d = n % ND;
-                o[d] = mfma32<DT>(vf[n % kAhead], pf[e & 1], o[d]);
-                if constexpr (n + kAhead < 4 * ND) vf[n % kAhead] = v_read(n + kAhead);
-                if constexpr (e < 3) {
-#pragma unroll
-                    for (int w = 4 / ND * d; w < 4 / ND * (d + 1); ++w) exps(e + 1, w);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            });
-            l += sum[0] + sum[1];
+                pf[2 * kt + (i >> 3)][(i >> 1) & 3] = pack16bit<DT>(a, b);
+            }
+        l += sum[0] + sum[1];
+    };
+
+    // Two groups of waves, four each, one wave of either on every SIMD, half a step apart: while one group multiplies, the other
+    // has its softmax, so that the matrix cores and the vector unit work side by side.  A barrier ends each half.  With the first
+    // group's products of step j begin the loads of the keys of step j + 1 and the values of step j (everybody is past the
+    // buffers that they go to); they are waited for before the half in which the first group needs them.
+    const int steps = step1 - step0;
+    const bool second = wave >= W / 2, works = wave_rows > 0;      // (a wave without rows only helps to load)
+    u32 unit = ~0u;                                           // rows of the step whose values are loaded next
+    uint64_t seen = 0, seen_before = 0;
+    auto issue = [&](int j) {                                  // keys of step j + 1, values of step j
+        const u32 next = answer();
+        ask(step0 + j + 2);
+        seen_before = seen;
+        seen = __builtin_amdgcn_ballot_w64(next != ~0u);
+        if (j + 1 < steps) load(next, ~seen == 0, (j + 1) & 1, K);
+        load(unit, ~seen_before == 0, j & 1, V);
+        unit = next;
+    };
+    auto arrive = [&](int j) {                                 // ends the half before the products of step j + 1
+        if constexpr (C8) {
+            if (j + 1 < steps) widen_to_lds((j + 1) & 1, K);
+            widen_to_lds(j & 1, V);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+    };
+    auto barrier = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    const std::integral_constant<bool, true> yes;
+    const std::integral_constant<bool, false> no;
+    if (steps > 0) {
+        ask(step0);
+        unit = answer();
+        ask(step0 + 1);
+        seen = __builtin_amdgcn_ballot_w64(unit != ~0u);
+        load(unit, ~seen == 0, 0, K);
+        if constexpr (C8) {
+            widen_to_lds(0, K);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        barrier();
+        if (second) {
+            issue(0);
+            barrier();
+            if (works) products(no, yes, nullptr, smem);
+            arrive(0);
+            barrier();
+            for (int j = 1; j < steps; ++j) {
+                const uint64_t now = seen_before;
+                issue(j);
+                if (works) softmax(step0 + j - 1, now);
+                barrier();
+                if (works) products(yes, yes, smem + (2 + ((j - 1) & 1)) * kBuf, smem + (j & 1) * kBuf);
+                arrive(j);
+                barrier();
+            }
+            if (works) {
+                softmax(step0 + steps - 1, seen_before);
+                products(yes, no, smem + (2 + ((steps - 1) & 1)) * kBuf, nullptr);
+            }
+        } else {
+            issue(0);
+            if (works) products(no, yes, nullptr, smem);
+            barrier();
+            for (int j = 1; j < steps; ++j) {
+                if (works) softmax(step0 + j - 1, seen_before);
+                arrive(j - 1);
+                barrier();
+                issue(j);
+                if (works) products(yes, yes, smem + (2 + ((j - 1) & 1)) * kBuf, smem + (j & 1) * kBuf);
+                barrier();
+            }
+            if (works) softmax(step0 + steps - 1, seen_before);
+            arrive(steps - 1);
+            barrier();
+            if (works) products(yes, no, smem + (2 + ((steps - 1) & 1)) * kBuf, nullptr);
         }
     }
     {
@@ -651,9 +731,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
 
 template <int DT, bool C8, int DH>
 hipError_t launch(PagedParams &p, bool tiled, hipStream_t stream) {
-    p.tiles = (int)(p.tokens * p.group / (tiled ? kTileRows : kRows)) + p.seqs;
+    constexpr int W = 8;
+    p.tiles = (int)(p.tokens * p.group / (tiled ? 32 * W : kRows)) + p.seqs;
     const dim3 grid((u32)((int64_t)p.tiles * p.kv_heads * p.splits));
-    if (tiled) hipLaunchKernelGGL((paged_tiles_kernel<DT, C8, DH>), grid, dim3(256), 0, stream, p);
+    if (tiled) hipLaunchKernelGGL((paged_tiles_kernel<DT, C8, DH, W>), grid, dim3(64 * W), 0, stream, p);
     else hipLaunchKernelGGL((paged_rows_kernel<DT, C8, DH>), grid, dim3(kWaves * 64), 0, stream, p);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
@@ -671,7 +752,7 @@ bool wants_tiles(int64_t tokens, int seqs, int group) { return tokens * group > 
 int paged_splits(int64_t tokens, int seqs, int q_heads, int kv_heads, int head_dim, int64_t max_kv) {
     const int group = q_heads / kv_heads;
     const bool tiled = wants_tiles(tokens, seqs, group);
-    const int64_t blocks = (tokens * group / (tiled ? kTileRows : kRows) + seqs) * kv_heads;
+    const int64_t blocks = (tokens * group / (tiled ? 256 : kRows) + seqs) * kv_heads;
     // enough workgroups for the chip, each with at least two steps per wave (tiles: four steps)
     const int64_t want = ((tiled ? 512 : 1024) + blocks - 1) / blocks;
     const int64_t most = max_kv / 256;
