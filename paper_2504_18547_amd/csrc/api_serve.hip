@@ -210,8 +210,10 @@ vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64
     // an `out` that overlaps q must be q: the rows are read and written by the same workgroup
     if (q == out && q_ld != out_ld) return VQ_ERR_STRIDE;
     if (max_kv == 0) max_kv = (int64_t)table_cols * cache->page_size;
+    // (a window shortens what a tile of rows sees; the workspace, which knows of none, is then more than enough)
+    const int64_t longest = window > 0 && window + 256 < max_kv ? window + 256 : max_kv;
     vitq::PagedParams p{};
-    p.splits = vitq::paged_splits(tokens, seqs, q_heads, cache->heads, cache->head_dim, max_kv);
+    p.splits = vitq::paged_splits(tokens, seqs, q_heads, cache->heads, cache->head_dim, longest);
     const size_t need = split_bytes(p.splits, tokens, q_heads, cache->head_dim);
     if (need > 0) {
         if (!workspace || workspace_bytes < need) return VQ_ERR_WORKSPACE;
@@ -240,7 +242,7 @@ vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64
     p.v_scale = cache->v_scale;
     p.causal = causal ? 1 : 0; p.window = window;
     p.out = (uint8_t *)out; p.out_ld = out_ld; p.lse = lse;
-    return vitq::paged_launch(p, dtype, cache->dtype, cache->head_dim, (hipStream_t)stream) == hipSuccess ? VQ_OK : VQ_ERR_HIP;
+    return vitq::paged_launch(p, dtype, cache->dtype, cache->head_dim, longest, (hipStream_t)stream) == hipSuccess ? VQ_OK : VQ_ERR_HIP;
 }
 
 }  // extern "C"

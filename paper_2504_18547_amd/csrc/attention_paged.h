@@ -20,12 +20,14 @@ struct PagedParams {
     int negative;                                             // the scale is negative
     int causal, window;
     uint8_t *out; int64_t out_ld; float *lse;
-    int tiles;                                                // of rows, over all sequences (set by the launcher)
     int splits; float *part, *part_lse;                       // [split][token][head][head_dim], [split][token][head]
+    // set by the launcher: keys of a split, row tiles over all sequences, rows up to which a sequence is the streaming form's
+    int split_keys, row_tiles; int64_t few_rows;
 };
 
 // Splits of the keys that the launcher chooses for these sizes (1: no workspace).
 int paged_splits(int64_t tokens, int seqs, int q_heads, int kv_heads, int head_dim, int64_t max_kv);
-hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, hipStream_t stream);
+// longest: keys that a row tile may see, as far as the host knows
+hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, int64_t longest, hipStream_t stream);
 
 }  // namespace vitq

@@ -6,6 +6,9 @@
 // (S^T = K Q^T): a lane of the result holds keys of ONE row, the softmax statistics are per lane, and the probabilities are
 // already the B operand of O^T = V^T P^T, whose order of keys is that of the score registers.
 #include "attention_paged.h"
+
+#include <algorithm>
+
 #include "serve_dev.h"
 
 namespace vitq {
@@ -41,7 +44,8 @@ __device__ __forceinline__ int64_t clamp_offset(const PagedParams &p, int s) {
     return o < 0 ? 0 : (o > p.tokens ? p.tokens : o);
 }
 
-template <int ROWS>
+// false: no such tile, or its sequence belongs to the other form (FEW: up to p.few_rows rows)
+template <int ROWS, bool FEW>
 __device__ __forceinline__ bool find_tile(const PagedParams &p, int tile, RowTile &t) {
     const int lane = threadIdx.x & 63;
     int lo = 0, n = p.seqs;
@@ -60,13 +64,36 @@ __device__ __forceinline__ bool find_tile(const PagedParams &p, int tile, RowTil
     t.seq = lo; t.first = (int)first; t.count = (int)(end - first);
     if (tile < tile0 || t.count <= 0) return false;
     const int64_t row0 = (tile - tile0) * ROWS, rows = (int64_t)t.count * p.group;
-    if (row0 >= rows) return false;
+    if (row0 >= rows || (rows <= p.few_rows) != FEW) return false;
     t.row0 = (int)row0;
     t.rows = (int)min((int64_t)ROWS, rows - row0);
     const int64_t most = (int64_t)p.table_cols * p.page_size;
     const int64_t kv = p.kv_lens[lo];
     t.kv_len = (int)(kv < 0 ? 0 : (kv > most ? most : kv));
     return true;
+}
+
+// Which tile, head and split a workgroup has.  Workgroups go round-robin to the eight XCDs, each with an L2 of its own.
+// RUNS: one XCD has a run of consecutive tiles of one head and split, which share keys; the last tiles, which see most under a
+// causal mask, start first.  Else splits, then heads, then tiles: evenly spread whatever the lengths (and tiles of one sequence are
+// a multiple of eight apart where heads or splits are).
+template <bool RUNS>
+__device__ __forceinline__ int tile_of_block(const PagedParams &p, int &head, int &split) {
+    // (the divisions run on the vector unit: back to scalars)
+    const int block = blockIdx.x;
+    if constexpr (!RUNS) {
+        const int rest = __builtin_amdgcn_readfirstlane(block / p.splits), tile = __builtin_amdgcn_readfirstlane(rest / p.kv_heads);
+        split = block - rest * p.splits;
+        head = rest - tile * p.kv_heads;
+        return tile;
+    } else {
+        const int total = gridDim.x, xcd = block & 7, slot = block >> 3, per = total >> 3, rem = total & 7;
+        const int id = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + slot;
+        const int unit = __builtin_amdgcn_readfirstlane(id / p.row_tiles);
+        split = __builtin_amdgcn_readfirstlane(unit / p.kv_heads);
+        head = unit - split * p.kv_heads;
+        return p.row_tiles - 1 - (id - unit * p.row_tiles);
+    }
 }
 
 // keys [lo, hi) that the row of token i of a sequence sees
@@ -86,7 +113,7 @@ __device__ __forceinline__ void row_range(const PagedParams &p, const RowTile &t
 constexpr int kRows = 16, kStep = 32, kWaves = 4;
 
 template <int DT, bool C8, int DH>
-__global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedParams p) {
+__global__ __launch_bounds__(kWaves * 64, DH == 64 ? 4 : 2) void paged_rows_kernel(const PagedParams p) {
     constexpr int NQ = DH / 32;                               // contraction steps of 32 channels
     constexpr int NT = DH / 16;                               // 16-channel tiles of the output
     constexpr int ND = DH / 32;                               // words of two channels that a lane holds of a V row
@@ -96,11 +123,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, q4 = lane >> 4;
-    const int split = blockIdx.x % p.splits;
-    const int rest = blockIdx.x / p.splits;
-    const int head = rest % p.kv_heads;
+    int head, split;
+    const int tile = tile_of_block<false>(p, head, split);
     RowTile t;
-    if (!find_tile<kRows>(p, rest / p.kv_heads, t)) return;
+    if (!find_tile<kRows, true>(p, tile, t)) return;
 
     // this lane's row
     const int r = min(l16, t.rows - 1) + t.row0;
@@ -113,10 +139,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
         row_range(p, t, tb, last_lo, hi);
     }
     const int lowest = lo;
+    const u32 my_span = (u32)(my_hi - my_lo);
     lo &= ~(kStep - 1);
     const int all_steps = hi > lo ? (hi - lo + kStep - 1) / kStep : 0;
-    const int per = (all_steps + p.splits - 1) / p.splits;
-    const int step0 = split * per, step1 = min(all_steps, step0 + per);
+    const int step0 = split * (p.split_keys / kStep), step1 = split + 1 == p.splits ? all_steps : min(all_steps, step0 + p.split_keys / kStep);
 
     v4u qf[NQ];
     {
@@ -136,53 +162,38 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
     for (int i = 0; i < NT; ++i) o[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
 
-    for (int st = step0 + wave; st < step1; st += kWaves) {
-        const int key0 = lo + st * kStep;
-        // each lane finds one key's row (the upper half repeats the lower)
-        const int key = key0 + (lane & 31);
-        u32 unit = head_unit;
-        bool there = key >= lowest && key < hi;
-        if (there) {
-            const u32 pg = divide((u32)key, p.page_div);
-            const u32 page = (u32)table[pg];
-            there = page < p.pages;
-            if (there) unit += page * p.page_units + ((u32)key - pg * p.page_size) * p.token_units;
-        }
-        const u32 seen = (u32)__builtin_amdgcn_ballot_w64(there);        // bit i: some row sees key0 + i, and it is in the cache
-        v4u kf[2][KL];
+    // A step's operands as they lie in the cache.  They are requested a step before they are used, and their page numbers a step
+    // before that: a wave has one step's keys and values in flight while it works on another's.
+    typedef u32 VRow __attribute__((ext_vector_type(C8 ? ND / 2 : ND)));
+    struct Operands { v4u k[2][KL]; VRow v[8]; u32 seen; };    // bit i of seen: some row sees key i of the step, and it is in the cache
+    u32 asked_page = ~0u, asked_place = ~0u;
+    // (each lane looks after one key; the upper half repeats the lower)
+    auto ask = [&](int st) {
+        const int key = lo + st * kStep + (lane & 31);
+        const bool want = st < step1 && key >= lowest && key < hi;
+        const u32 pg = divide((u32)(want ? key : lowest), p.page_div);
+        asked_page = (u32)table[pg];                          // (some page of this sequence where the lane has no key)
+        asked_place = want ? (u32)key - pg * p.page_size : ~0u;
+    };
+    auto fetch = [&](Operands &x) {
+        const bool there = asked_place != ~0u && asked_page < p.pages;
+        const u32 unit = head_unit + (there ? asked_page * p.page_units + asked_place * p.token_units : 0u);
+        x.seen = (u32)__builtin_amdgcn_ballot_w64(there);
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
             const u32 u = (u32)__shfl((int)unit, tt * 16 + l16);
             const uint8_t *row = p.k + (uint64_t)u * 16 + 16 * q4;
 #pragma unroll
-            for (int i = 0; i < KL; ++i) kf[tt][i] = *reinterpret_cast<const v4u *>(row + 64 * i);
+            for (int i = 0; i < KL; ++i) x.k[tt][i] = *reinterpret_cast<const v4u *>(row + 64 * i);
         }
-        u32 vw[8][ND];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const u32 u = (u32)__shfl((int)unit, (j >> 2) * 16 + 4 * q4 + (j & 3));
-            if constexpr (C8) {
-                const uint8_t *at = p.v + (uint64_t)u * 16 + l16 * (2 * ND);
-                if constexpr (DH == 128) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(at);
-                    vw[j][0] = widen<DT, false>(w.x); vw[j][1] = widen<DT, true>(w.x);
-                    vw[j][2] = widen<DT, false>(w.y); vw[j][3] = widen<DT, true>(w.y);
-                } else {
-                    const u32 w = *reinterpret_cast<const u32 *>(at);
-                    vw[j][0] = widen<DT, false>(w); vw[j][1] = widen<DT, true>(w);
-                }
-            } else {
-                const uint8_t *at = p.v + (uint64_t)u * 16 + l16 * (4 * ND);
-                if constexpr (DH == 128) {
-                    const v4u w = *reinterpret_cast<const v4u *>(at);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) vw[j][i] = w[i];
-                } else {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(at);
-                    vw[j][0] = w.x; vw[j][1] = w.y;
-                }
-            }
+            x.v[j] = *reinterpret_cast<const VRow *>(p.v + (uint64_t)u * 16 + l16 * sizeof(VRow));
         }
+    };
+    auto work = [&](Operands &x, int st) {
+        const int key0 = lo + st * kStep;
         // scores: register i of tile tt is key 16 tt + 4 q4 + i of this lane's row
         float s[8];
 #pragma unroll
@@ -191,32 +202,24 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 v4u f;
-                if constexpr (C8) {
-                    const u32 w0 = kf[tt][i >> 1][(i & 1) * 2], w1 = kf[tt][i >> 1][(i & 1) * 2 + 1];
-                    f[0] = widen<DT, false>(w0); f[1] = widen<DT, true>(w0);
-                    f[2] = widen<DT, false>(w1); f[3] = widen<DT, true>(w1);
-                } else {
-                    f = kf[tt][i];
-                }
+                if constexpr (C8) f = widen8<DT>(x.k[tt][i >> 1][(i & 1) * 2], x.k[tt][i >> 1][(i & 1) * 2 + 1]);
+                else f = x.k[tt][i];
                 a = mfma16<DT>(f, qf[i], a);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[4 * tt + i] = a[i] * p.scale_log2;
         }
-        if (seen != 0xFFFFFFFFu || key0 < last_lo || key0 + kStep > first_hi) {
+        if (x.seen != 0xFFFFFFFFu || key0 < last_lo || key0 + kStep > first_hi) {
+            const u32 mine = x.seen >> (4 * q4);
+            const int first = key0 + 4 * q4 - my_lo;              // this lane's key 0 against what its row sees
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int at = (i >> 2) * 16 + 4 * q4 + (i & 3);
-                const bool on = ((seen >> at) & 1u) && key0 + at >= my_lo && key0 + at < my_hi;
-                s[i] = on ? s[i] : -INFINITY;
+                const int at = (i >> 2) * 16 + (i & 3);
+                const bool there = (mine & (1u << at)) != 0;
+                s[i] = there && (u32)(first + at) < my_span ? s[i] : -INFINITY;
+                // what is not in the cache must not reach the sums, not even times zero
+                if (!there) x.v[i] = 0;
             }
-            // what is not in the cache must not reach the sums, not even times zero
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (!((seen >> ((j >> 2) * 16 + 4 * q4 + (j & 3))) & 1u)) {
-#pragma unroll
-                    for (int i = 0; i < ND; ++i) vw[j][i] = 0;
-                }
         }
         float top = s[0];
 #pragma unroll
@@ -239,14 +242,38 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(const PagedPara
         for (int i = 0; i < NT; ++i) o[i] *= alpha;
 #pragma unroll
         for (int w = 0; w < ND; ++w) {
+            u32 row[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (C8) row[j] = (w & 1) ? widen<DT, true>(x.v[j][w >> 1]) : widen<DT, false>(x.v[j][w >> 1]);
+                else row[j] = x.v[j][w];
+            }
             v4u a, b;
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj) {
-                a[jj] = __builtin_amdgcn_perm(vw[2 * jj + 1][w], vw[2 * jj][w], 0x05040100u);
-                b[jj] = __builtin_amdgcn_perm(vw[2 * jj + 1][w], vw[2 * jj][w], 0x07060302u);
+                a[jj] = __builtin_amdgcn_perm(row[2 * jj + 1], row[2 * jj], 0x05040100u);
+                b[jj] = __builtin_amdgcn_perm(row[2 * jj + 1], row[2 * jj], 0x07060302u);
             }
             o[2 * w] = mfma16<DT>(a, pf, o[2 * w]);
             o[2 * w + 1] = mfma16<DT>(b, pf, o[2 * w + 1]);
+        }
+    };
+    {
+        int st = step0 + wave;
+        if (st < step1) {
+            Operands x, y;
+            ask(st);
+            fetch(x);
+            ask(st + kWaves);
+            for (; st < step1; st += 2 * kWaves) {
+                if (st + kWaves < step1) fetch(y);
+                ask(st + 2 * kWaves);
+                work(x, st);
+                if (st + kWaves >= step1) break;
+                if (st + 2 * kWaves < step1) fetch(x);
+                ask(st + 3 * kWaves);
+                work(y, st + kWaves);
+            }
         }
     }
     l = sum_quarters(l);
@@ -346,19 +373,10 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h = lane >> 5;
 
-    // Workgroups go round-robin to the eight XCDs; one XCD gets consecutive numbers, and those are row tiles of one head: they
-    // share its keys in that L2.  The last tiles, which see most under a causal mask, start first.
-    int id;
-    {
-        const int total = gridDim.x, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = total >> 3, rem = total & 7;
-        id = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + slot;
-    }
-    const int tiles = p.tiles;
-    const int rest = (int)__builtin_amdgcn_readfirstlane(id / tiles);
-    const int tile = tiles - 1 - (id - rest * tiles);
-    const int split = (int)__builtin_amdgcn_readfirstlane(rest / p.kv_heads), head = rest - split * p.kv_heads;
+    int head, split;
+    const int tile = tile_of_block<true>(p, head, split);
     RowTile t;
-    if (!find_tile<kTileRows>(p, tile, t)) return;
+    if (!find_tile<kTileRows, false>(p, tile, t)) return;
 
     // this lane's row, and what the wave's rows see
     const int wave_rows = min(32, t.rows - 32 * wave);        // may be <= 0: the wave only helps to load
@@ -377,8 +395,7 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
     const int lowest = lo;
     lo &= ~(kTileKeys - 1);
     const int all_steps = hi > lo ? (hi - lo + kTileKeys - 1) / kTileKeys : 0;
-    const int per = (all_steps + p.splits - 1) / p.splits;
-    const int step0 = split * per, step1 = min(all_steps, step0 + per);
+    const int step0 = split * (p.split_keys / kTileKeys), step1 = split + 1 == p.splits ? all_steps : min(all_steps, step0 + p.split_keys / kTileKeys);
 
     // Q: channels 16 i + 8 h .. of this lane's row; a negative scale is a sign of the queries (maxima are taken before scaling)
     v4u qf[NQ];
@@ -691,36 +708,81 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
 }
 
 // ---- joins the splits of a row: a weighted mean with weights exp2(lse_split - the largest) --------------------------------
+// Sixteen lanes have the channels of a row; `1 << lanes_log2` such groups share its splits and are joined in LDS.
 template <int DT, int DH>
-__global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p, int groups_log2) {
     constexpr int CH = DH / 16;
+    __shared__ __attribute__((aligned(16))) float part[16][DH + 4];
+    __shared__ float part_m[16], part_l[16];
     const int64_t rows = p.tokens * p.q_heads;
-    const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    if (at >= rows) return;
+    const int group = threadIdx.x >> 4, groups = 1 << groups_log2, mine = group & (groups - 1);
+    const int64_t at = ((int64_t)blockIdx.x << (4 - groups_log2)) + (group >> groups_log2);
     const int64_t token = at / p.q_heads;
-    if (token < clamp_offset(p, 0) || token >= clamp_offset(p, p.seqs)) return;      // a row outside every sequence
+    const bool live = at < rows && token >= clamp_offset(p, 0) && token < clamp_offset(p, p.seqs);      // (a row of a sequence)
     const int c = (threadIdx.x & 15) * CH;
-    float best = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) best = fmaxf(best, p.part_lse[s * rows + at]);
-    const float base = best == -INFINITY ? 0.0f : best;
-    float total = 0.0f, y[CH];
+    float m = -INFINITY, l = 0.0f, y[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) y[i] = 0.0f;
-    for (int s = 0; s < p.splits; ++s) {
-        const float lse = p.part_lse[s * rows + at];
-        if (lse == -INFINITY) continue;                          // nothing was written for it
-        const float f = __builtin_amdgcn_exp2f(lse - base);
-        total += f;
-        const float *src = p.part + (s * rows + at) * DH + c;
+    if (live) {
+        constexpr int U = 4;                                     // splits whose loads are in flight together
+        for (int s0 = mine; s0 < p.splits; s0 += groups * U) {
+            float lse[U];
+            v4f v[U][CH / 4];
 #pragma unroll
-        for (int i = 0; i < CH; i += 4) {
-            const v4f v = *reinterpret_cast<const v4f *>(src + i);
+            for (int u = 0; u < U; ++u) {
+                const int s = s0 + u * groups;
+                lse[u] = s < p.splits ? p.part_lse[s * rows + at] : -INFINITY;
+            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[i + j] = fmaf(v[j], f, y[i + j]);
+            for (int u = 0; u < U; ++u) {
+                const int s = s0 + u * groups;
+                // (where nothing is seen nothing was written either)
+#pragma unroll
+                for (int i = 0; i < CH / 4; ++i)
+                    v[u][i] = lse[u] != -INFINITY ? *reinterpret_cast<const v4f *>(p.part + (s * rows + at) * DH + c + 4 * i) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            float top = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, lse[u]);
+            const float base = top == -INFINITY ? 0.0f : top;
+            const float keep = __builtin_amdgcn_exp2f(m - base);
+            m = top;
+            l *= keep;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) y[i] *= keep;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float f = __builtin_amdgcn_exp2f(lse[u] - base);
+                l += f;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) y[i] = fmaf(v[u][i >> 2][i & 3], f, y[i]);
+            }
         }
     }
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    if (c == 0 && p.lse) p.lse[at] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * 0x1.62e430p-1f;
+    if (groups > 1) {
+#pragma unroll
+        for (int i = 0; i < CH; i += 4) *reinterpret_cast<v4f *>(&part[group][c + i]) = v4f{y[i], y[i + 1], y[i + 2], y[i + 3]};
+        if (c == 0) { part_m[group] = m; part_l[group] = l; }
+        __syncthreads();
+        if (!live || mine != 0) return;
+        float top = m;
+        for (int o = 1; o < groups; ++o) top = fmaxf(top, part_m[group + o]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        const float keep = __builtin_amdgcn_exp2f(m - base);
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) y[i] *= keep;
+        for (int o = 1; o < groups; ++o) {
+            const float f = __builtin_amdgcn_exp2f(part_m[group + o] - base);
+            l = fmaf(part_l[group + o], f, l);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) y[i] = fmaf(part[group + o][c + i], f, y[i]);
+        }
+        m = top;
+    }
+    if (!live) return;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (c == 0 && p.lse) p.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0x1.62e430p-1f;
     u32 w[CH / 2];
 #pragma unroll
     for (int i = 0; i < CH / 2; ++i) w[i] = pack16bit<DT>(y[2 * i] * inv, y[2 * i + 1] * inv);
@@ -729,42 +791,73 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedParams p) {
     for (int i = 0; i < CH / 2; i += 2) *reinterpret_cast<uint2 *>(d + i) = make_uint2(w[i], w[i + 1]);
 }
 
+constexpr int kFewRows = 64, kWgRows = 256;
+
+// Which forms a batch needs; the host knows the totals alone.  A mean above kFewRows rows a sequence: tiles.  Below it the
+// streaming form, and both where one sequence can have a chunk of four tiles and more beside single tokens (each form then
+// passes over the other's sequences).
+struct Forms { bool few, many; };
+Forms forms_of(int64_t tokens, int seqs, int group) {
+    if (tokens * group > (int64_t)kFewRows * seqs) return Forms{false, true};
+    return Forms{true, (tokens - seqs + 1) * group >= 4 * kWgRows};
+}
+
 template <int DT, bool C8, int DH>
-hipError_t launch(PagedParams &p, bool tiled, hipStream_t stream) {
-    constexpr int W = 8;
-    p.tiles = (int)(p.tokens * p.group / (tiled ? 32 * W : kRows)) + p.seqs;
-    const dim3 grid((u32)((int64_t)p.tiles * p.kv_heads * p.splits));
-    if (tiled) hipLaunchKernelGGL((paged_tiles_kernel<DT, C8, DH, W>), grid, dim3(64 * W), 0, stream, p);
-    else hipLaunchKernelGGL((paged_rows_kernel<DT, C8, DH>), grid, dim3(kWaves * 64), 0, stream, p);
-    hipError_t e = hipGetLastError();
+hipError_t launch(PagedParams &p, hipStream_t stream) {
+    const Forms f = forms_of(p.tokens, p.seqs, p.group);
+    p.few_rows = !f.many ? INT64_MAX : (f.few ? kFewRows : -1);
+    hipError_t e = hipSuccess;
+    if (f.many) {
+        p.row_tiles = (int)(p.tokens * p.group / kWgRows) + p.seqs;
+        hipLaunchKernelGGL((paged_tiles_kernel<DT, C8, DH, kWgRows / 32>), dim3((u32)((int64_t)p.row_tiles * p.kv_heads * p.splits)), dim3(2 * kWgRows), 0, stream, p);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && f.few) {
+        p.row_tiles = (int)(p.tokens * p.group / kRows) + p.seqs;
+        hipLaunchKernelGGL((paged_rows_kernel<DT, C8, DH>), dim3((u32)((int64_t)p.row_tiles * p.kv_heads * p.splits)), dim3(kWaves * 64), 0, stream, p);
+        e = hipGetLastError();
+    }
     if (e == hipSuccess && p.splits > 1) {
-        hipLaunchKernelGGL((paged_join_kernel<DT, DH>), dim3((u32)((p.tokens * p.q_heads + 15) / 16)), dim3(256), 0, stream, p);
+        const int groups_log2 = p.splits <= 4 ? 0 : (p.splits <= 16 ? 2 : 4);
+        const int64_t rows = p.tokens * p.q_heads, per = 16 >> groups_log2;
+        hipLaunchKernelGGL((paged_join_kernel<DT, DH>), dim3((u32)((rows + per - 1) / per)), dim3(256), 0, stream, p, groups_log2);
         e = hipGetLastError();
     }
     return e;
 }
 
-// Rows per sequence decide: up to two sixteens, the form that streams the cache without LDS.
-bool wants_tiles(int64_t tokens, int seqs, int group) { return tokens * group > (int64_t)32 * seqs; }
-
 }  // namespace
 
 int paged_splits(int64_t tokens, int seqs, int q_heads, int kv_heads, int head_dim, int64_t max_kv) {
     const int group = q_heads / kv_heads;
-    const bool tiled = wants_tiles(tokens, seqs, group);
-    const int64_t blocks = (tokens * group / (tiled ? 256 : kRows) + seqs) * kv_heads;
-    // enough workgroups for the chip, each with at least two steps per wave (tiles: four steps)
-    const int64_t want = ((tiled ? 512 : 1024) + blocks - 1) / blocks;
-    const int64_t most = max_kv / 256;
-    int64_t s = want < most ? want : most;
-    return s < 1 ? 1 : (s > 64 ? 64 : (int)s);
+    const Forms f = forms_of(tokens, seqs, group);
+    int64_t s = 1;
+    auto at_least = [&](int64_t n) { s = n > s ? n : s; };
+    if (f.few) {
+        // A round of workgroups with as little as 256 keys each; more rounds, which even out unequal lengths, only of longer
+        // pieces (a piece costs its prologue and its way through the workspace).  us, 256 / 512 / 1024 keys a piece: one token,
+        // 16,384 keys 19.8 / 19.0 / 21.9; eight, 8,192 keys 59.9 / 55.9 / 54.1; 16 x 8 over 4,096 78.0 / 78.3 / 68.2.
+        const int64_t blocks = (tokens * group / kRows + seqs) * kv_heads;
+        at_least(std::min(512 / blocks, max_kv / 256));
+        at_least(std::min(1024 / blocks, max_kv / 512));
+        at_least(std::min(4096 / blocks, max_kv / 1024));
+    }
+    if (f.many) {
+        // a workgroup per CU: 64 rows x 4 over 16,384 keys 42.7 us, with twice as many 57.5, four times 78.5
+        const int64_t blocks = (tokens * group / kWgRows + (f.few ? 1 : seqs)) * kv_heads;
+        at_least(std::min(256 / blocks, max_kv / 256));
+    }
+    return (int)std::min<int64_t>(s, 64);
 }
 
-hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, hipStream_t stream) {
-    const bool c8 = cache_dtype == kE4M3, tiled = wants_tiles(p.tokens, p.seqs, p.group);
+hipError_t paged_launch(PagedParams p, int dtype, int cache_dtype, int head_dim, int64_t longest, hipStream_t stream) {
+    // equal pieces of the longest range, whole steps of either form; the last one takes what a longer sequence has left
+    p.split_keys = (int)(((longest + p.splits - 1) / p.splits + 63) / 64 * 64);
+    if (p.split_keys < 64) p.split_keys = 64;
+    const bool c8 = cache_dtype == kE4M3;
 #define VITQ_PAGED(DT) \
-    if (head_dim == 64) return c8 ? launch<DT, true, 64>(p, tiled, stream) : launch<DT, false, 64>(p, tiled, stream); \
-    return c8 ? launch<DT, true, 128>(p, tiled, stream) : launch<DT, false, 128>(p, tiled, stream);
+    if (head_dim == 64) return c8 ? launch<DT, true, 64>(p, stream) : launch<DT, false, 64>(p, stream); \
+    return c8 ? launch<DT, true, 128>(p, stream) : launch<DT, false, 128>(p, stream);
     if (dtype == kBF16) { VITQ_PAGED(kBF16) }
     VITQ_PAGED(kF16)
 #undef VITQ_PAGED
