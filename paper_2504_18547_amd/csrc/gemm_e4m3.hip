@@ -90,11 +90,8 @@ __device__ __forceinline__ void store8_16bit(const GemmE4M3Params &p, int m, int
     }
 }
 
-__device__ __forceinline__ v8i operand(const uint4 &a, const uint4 &b) {
-    v8i r;
-    r[0] = (int)a.x; r[1] = (int)a.y; r[2] = (int)a.z; r[3] = (int)a.w;
-    r[4] = (int)b.x; r[5] = (int)b.y; r[6] = (int)b.z; r[7] = (int)b.w;
-    return r;
+__device__ __forceinline__ v8i operand(const v4i &a, const v4i &b) {
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // ---- few rows or few tiles: the waves of a workgroup share K ------------------------------------------------------------
@@ -109,15 +106,19 @@ __global__ __launch_bounds__(1024) void gemm_e4m3_split_kernel(const GemmE4M3Par
     const int l16 = lane & 15, q = lane >> 4;
     const int c0 = blockIdx.x * (16 * AT), t0 = blockIdx.y * (16 * TT);
     const int nk = (p.K + 127) >> 7;
-    const uint8_t *wrow[AT], *xrow[TT];
+    // rows beyond the matrix and chunks beyond the padded row read as zeros
+    const auto wbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.w + (int64_t)c0 * p.w_stride), 0,
+                                                        (u32)(min(16 * AT, p.Nout - c0) - 1) * (u32)p.w_stride + (u32)p.kbytes16, 0x00020000);
+    const auto xbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p.x + (int64_t)t0 * p.x_stride), 0,
+                                                        (u32)(min(16 * TT, p.M - t0) - 1) * (u32)p.x_stride + (u32)p.kbytes16, 0x00020000);
+    u32 wrow[AT], xrow[TT];
     const float *xsc[TT];
 #pragma unroll
-    for (int a = 0; a < AT; ++a) wrow[a] = p.w + (int64_t)min(c0 + 16 * a + l16, p.Nout - 1) * p.w_stride + 16 * q;
+    for (int a = 0; a < AT; ++a) wrow[a] = (u32)(16 * a + l16) * (u32)p.w_stride;
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
-        const int m = min(t0 + 16 * t + l16, p.M - 1);
-        xrow[t] = p.x + (int64_t)m * p.x_stride + 16 * q;
-        xsc[t] = p.xs + m;
+        xrow[t] = (u32)(16 * t + l16) * (u32)p.x_stride;
+        xsc[t] = p.xs + min(t0 + 16 * t + l16, p.M - 1);
     }
     const float *wsc = p.ws + (c0 >> 7);
     v4f acc[AT][TT];
@@ -127,41 +128,42 @@ __global__ __launch_bounds__(1024) void gemm_e4m3_split_kernel(const GemmE4M3Par
         for (int t = 0; t < TT; ++t) acc[a][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
     for (int kb0 = wave; kb0 < nk; kb0 += nw * U) {
-        uint4 wv[U][AT][2], xv[U][TT][2];
-        float s[U][TT];
+        v4i wv[U][AT][2], xv[U][TT][2];
+        float sx[U][TT], sw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int kb = kb0 + u * nw;
-            if (kb < nk) {
-                // a chunk of 16 bytes lies wholly inside the padded row or wholly beyond it
-                const bool in0 = kb * 128 + 16 * q < p.kbytes16, in1 = kb * 128 + 64 + 16 * q < p.kbytes16;
-                const uint4 zero = make_uint4(0, 0, 0, 0);
+            const u32 at0 = (u32)(kb * 128 + 16 * q), at1 = at0 + 64;
+            // (a chunk of 16 bytes lies wholly inside the padded row or wholly beyond it)
+            const bool in0 = at0 < (u32)p.kbytes16, in1 = at1 < (u32)p.kbytes16;
 #pragma unroll
-                for (int a = 0; a < AT; ++a) {
-                    wv[u][a][0] = in0 ? *reinterpret_cast<const uint4 *>(wrow[a] + kb * 128) : zero;
-                    wv[u][a][1] = in1 ? *reinterpret_cast<const uint4 *>(wrow[a] + kb * 128 + 64) : zero;
-                }
-                const float sw = wsc[(int64_t)kb * p.ws_stride];
-#pragma unroll
-                for (int t = 0; t < TT; ++t) {
-                    xv[u][t][0] = in0 ? *reinterpret_cast<const uint4 *>(xrow[t] + kb * 128) : zero;
-                    xv[u][t][1] = in1 ? *reinterpret_cast<const uint4 *>(xrow[t] + kb * 128 + 64) : zero;
-                    s[u][t] = sw * xsc[t][(int64_t)kb * p.xs_stride];
-                }
+            for (int a = 0; a < AT; ++a) {
+                wv[u][a][0] = __builtin_amdgcn_raw_buffer_load_b128(wbuf, in0 ? wrow[a] + at0 : ~15u, 0, 0);
+                wv[u][a][1] = __builtin_amdgcn_raw_buffer_load_b128(wbuf, in1 ? wrow[a] + at1 : ~15u, 0, 0);
             }
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                xv[u][t][0] = __builtin_amdgcn_raw_buffer_load_b128(xbuf, in0 ? xrow[t] + at0 : ~15u, 0, 0);
+                xv[u][t][1] = __builtin_amdgcn_raw_buffer_load_b128(xbuf, in1 ? xrow[t] + at1 : ~15u, 0, 0);
+            }
+            const int64_t row = min(kb, nk - 1);               // (behind the last block the operands are zeros: any scale will do)
+            sw[u] = wsc[row * p.ws_stride];
+#pragma unroll
+            for (int t = 0; t < TT; ++t) sx[u][t] = xsc[t][row * p.xs_stride];
         }
+        __builtin_amdgcn_sched_barrier(0);                      // all loads are on their way before the first product
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (kb0 + u * nw < nk) {
+            if (kb0 + u * nw >= nk) break;                     // (a scale may be infinite or NaN: nothing is added behind the last)
 #pragma unroll
-                for (int a = 0; a < AT; ++a)
+            for (int a = 0; a < AT; ++a)
 #pragma unroll
-                    for (int t = 0; t < TT; ++t) {
-                        const v4f d = mfma_block<WIDE>(operand(wv[u][a][0], wv[u][a][1]), operand(xv[u][t][0], xv[u][t][1]));
+                for (int t = 0; t < TT; ++t) {
+                    const v4f d = mfma_block<WIDE>(operand(wv[u][a][0], wv[u][a][1]), operand(xv[u][t][0], xv[u][t][1]));
+                    const float s = sw[u] * sx[u][t];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[a][t][r] = fmaf(d[r], s[u][t], acc[a][t][r]);
-                    }
-            }
+                    for (int r = 0; r < 4; ++r) acc[a][t][r] = fmaf(d[r], s, acc[a][t][r]);
+                }
         }
     }
     constexpr int kTiles = AT * TT;
@@ -317,7 +319,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     const u32 p0 = (u32)((q ^ (l16 & 7)) * 16), p1 = (u32)(((q + 4) ^ (l16 & 7)) * 16);
     const u32 wrow = (u32)((wc * (16 * AT) + l16) * 128), xrow = (u32)((TC + wt * (16 * TT) + l16) * 128);
     auto frag = [&](const uint8_t *stage, u32 row) {
-        return operand(*reinterpret_cast<const uint4 *>(stage + row + p0), *reinterpret_cast<const uint4 *>(stage + row + p1));
+        return operand(*reinterpret_cast<const v4i *>(stage + row + p0), *reinterpret_cast<const v4i *>(stage + row + p1));
     };
     v8i xf[TT], wf[3];
     float sc[TT];
