@@ -275,6 +275,12 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     uint64_t sbase = 0;
     u32 sbytes = 0;
     int next_id = id, load_kt = 0;
+    u32 w_at = 0, x_at = 0;                                          // this lane's offsets; past the end beyond a ragged K
+    auto aim = [&]() {
+        const bool in = load_kt * 128 + (int)chunk < p.kbytes16;
+        w_at = in ? woff + (u32)load_kt * 128u : ~15u;
+        x_at = in ? xoff + (u32)load_kt * 128u : ~15u;
+    };
     auto point = [&](bool some) {                                    // descriptors of tile next_id (empty ones behind the last)
         int c0 = 0, t0 = 0;
         if (some) place(next_id, c0, t0);
@@ -286,22 +292,25 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
         for (int i = 0; i < kLoadsX; ++i) xbuf[i] = rows_descriptor(xbase + (u32)(kStep * i) * x_stride, rows_x - kStep * i, x_stride, p.kbytes16);
         sbase = (uint64_t)(uintptr_t)(p.xs + t0);
         sbytes = (u32)rows_x * 4u;
+        aim();
     };
     // part i of the loads of the cursor's stage into buffer `half`; the last part: the tokens' scales
     constexpr int kParts = kLoadsW + kLoadsX + 1;
     auto issue = [&](int half, auto I) {
         constexpr int i = decltype(I)::value;
         const u32 dst = lds0 + (u32)half * kStage + i * (kThreads * 16);
-        const bool in = load_kt * 128 + (int)chunk < p.kbytes16;
-        if constexpr (i < kLoadsW) to_lds16(in ? woff + (u32)load_kt * 128u : ~15u, wbuf[i], dst);
-        else if constexpr (i < kLoadsW + kLoadsX) to_lds16(in ? xoff + (u32)load_kt * 128u : ~15u, xbuf[i - kLoadsW], dst);
+        if constexpr (i < kLoadsW) to_lds16(w_at, wbuf[i], dst);
+        else if constexpr (i < kLoadsW + kLoadsX) to_lds16(x_at, xbuf[i - kLoadsW], dst);
         else {
             if (wave * 64 < TK)
-                to_lds4(threadIdx.x * 4u, descriptor(sbase + (uint64_t)load_kt * p.xs_stride * 4u, sbytes), lds0 - (u32)wave * 768u + (u32)half * kStage + (TC + TK) * 128);
+                to_lds4(threadIdx.x * 4u, descriptor(sbase, sbytes), lds0 - (u32)wave * 768u + (u32)half * kStage + (TC + TK) * 128);
+            sbase += (uint64_t)p.xs_stride * 4u;
             if (++load_kt == nk) {
                 load_kt = 0;
                 next_id += stride;
                 point(next_id < run1);
+            } else {
+                aim();
             }
         }
     };

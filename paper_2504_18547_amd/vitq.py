@@ -425,18 +425,22 @@ def _here(*tensors):
 
 
 def _rows_2d(t, what):
-    """(dtype code, leading dimension) of a tensor [rows, cols] whose rows are contiguous."""
-    _want(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), what + " must be [rows, cols] with contiguous rows")
-    _want(t.dtype in _DTYPES, what + " has a type the library does not take")
-    ld = t.stride(0)
-    return _DTYPES[t.dtype], (ld if t.shape[0] > 1 else max(ld, t.shape[1]))
+    """(dtype code, rows, columns, leading dimension) of a tensor [rows, cols] whose rows are contiguous."""
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(what + " has a type the library does not take")
+    if t.dim() != 2:
+        raise ValueError(what + " must be [rows, cols]")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(what + " must have contiguous rows")
+    return code, rows, cols, (ld if rows > 1 else max(ld, cols))
 
 
 def _vector(t, dtype, count, what):
-    if t is not None:
-        _want(t.dtype == dtype and t.dim() == 1 and t.is_contiguous() and (count is None or t.shape[0] == count),
-              "%s must be a contiguous %s vector%s" % (what, dtype, "" if count is None else " of %d" % count))
-    return t
+    if t is not None and (t.dtype != dtype or t.dim() != 1 or not t.is_contiguous() or (count is not None and t.shape[0] != count)):
+        raise ValueError("%s must be a contiguous %s vector%s" % (what, dtype, "" if count is None else " of %d" % count))
 
 
 class FMat:
@@ -474,6 +478,7 @@ class KvCache:
         _want(k.dtype in _DTYPES and k.stride(3) == 1, "channels must be contiguous, of a type the library takes")
         self.k, self.v = k, v
         pages, heads, page_size, head_dim = k.shape
+        self.head_dim = head_dim
         self._c = vq_kv_cache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], heads, head_dim, page_size, pages, k.stride(0),
                               k.stride(1), k.stride(2), float(k_scale), float(v_scale))
         self._ref = C.byref(self._c)
@@ -483,18 +488,19 @@ class KvCache:
 
 
 def vq_quantize_e4m3(x, out):
-    code, ld = _rows_2d(x, "x")
+    code, rows, cols, ld = _rows_2d(x, "x")
     _here(x, out.data, out.scales)
-    _check(lib().vq_quantize_e4m3(x.data_ptr(), code, x.shape[0], x.shape[1], ld, out._ref, _stream()), "vq_quantize_e4m3")
+    _check(lib().vq_quantize_e4m3(x.data_ptr(), code, rows, cols, ld, out._ref, _stream()), "vq_quantize_e4m3")
     return out
 
 
 def vq_linear_e4m3(x, w, bias, act, y):
-    code, ld = _rows_2d(y, "y")
-    _want(y.shape[0] == x.rows and y.shape[1] == w.rows, "y must be [rows of x, rows of w]")
-    _vector(bias, torch.float32, w.rows, "bias")
-    _here(x.data, w.data, bias, y)
-    _check(lib().vq_linear_e4m3(x._ref, w._ref, _ptr(bias), int(act), y.data_ptr(), code, ld, _stream()), "vq_linear_e4m3")
+    code, rows, cols, ld = _rows_2d(y, "y")
+    if rows != x.rows or cols != w.rows:
+        raise ValueError("y must be [rows of x, rows of w]")
+    _vector(bias, torch.float32, cols, "bias")
+    _here(x.data, x.scales, w.data, w.scales, bias, y)
+    _check(lib().vq_linear_e4m3(x._ref, w._ref, _ptr(bias), act, y.data_ptr(), code, ld, _stream()), "vq_linear_e4m3")
 
 
 _NORMS = {"none": 0, "rms": 1, "layer": 2}
@@ -520,21 +526,24 @@ def make_rotate_desc(q_heads, kv_heads, head_dim, norm="rms", q_gamma=None, q_be
         for t in (cos, sin):
             _want(t.dtype == torch.float32 and t.dim() == 2 and t.is_contiguous() and t.shape == cos.shape, "cos and sin must be contiguous fp32 [rows, rot_dim/2]")
         d.cos_table, d.sin_table, d.table_rows, d.rot_dim = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1]
-    d._keep = (q_gamma, q_beta, k_gamma, k_beta, cos, sin)
+    d._keep = tuple(t for t in (q_gamma, q_beta, k_gamma, k_beta, cos, sin) if t is not None)
+    d._cols = (q_heads * head_dim, (q_heads + 2 * kv_heads) * head_dim)
     d._ref = C.byref(d)
     return d
 
 
 def vq_qkv_norm_rotate(desc, qkv, positions, q_out, cache, slots):
-    code, ld = _rows_2d(qkv, "qkv")
-    tokens = qkv.shape[0]
-    _want(qkv.shape[1] == (desc.q_heads + 2 * desc.kv_heads) * desc.head_dim, "qkv must have a column per channel of every head")
+    code, tokens, cols, ld = _rows_2d(qkv, "qkv")
+    q_cols, all_cols = desc._cols
+    if cols != all_cols:
+        raise ValueError("qkv must have a column per channel of every head")
     _vector(positions, torch.int32, tokens, "positions")
     _vector(slots, torch.int64, tokens, "slots")
-    q_code, q_ld = 0, 0
+    q_code = q_ld = 0
     if q_out is not None:
-        q_code, q_ld = _rows_2d(q_out, "q_out")
-        _want(q_out.shape[0] == tokens and q_out.shape[1] == desc.q_heads * desc.head_dim, "q_out must be [tokens, q_heads*head_dim]")
+        q_code, q_rows, width, q_ld = _rows_2d(q_out, "q_out")
+        if q_rows != tokens or width != q_cols:
+            raise ValueError("q_out must be [tokens, q_heads*head_dim]")
     _here(qkv, positions, q_out, slots, None if cache is None else cache.k, *desc._keep)
     _check(lib().vq_qkv_norm_rotate(desc._ref, qkv.data_ptr(), code, tokens, ld, _ptr(positions), _ptr(q_out), q_code, q_ld,
                                     None if cache is None else cache._ref, _ptr(slots), _stream()), "vq_qkv_norm_rotate")
@@ -549,22 +558,27 @@ def vq_attention_paged_workspace(tokens, seqs, q_heads, cache, max_kv):
 
 
 def vq_attention_paged(q, q_offsets, kv_lens, page_table, cache, scale, causal, window, max_kv, out, lse, workspace):
-    code, ld = _rows_2d(q, "q")
-    out_code, out_ld = _rows_2d(out, "out")
-    tokens, cols = q.shape
-    _want(out.shape == q.shape and out_code == code, "out must be like q")
-    _want(cols % cache._c.head_dim == 0, "q must have a column per channel of every head")
-    q_heads = cols // cache._c.head_dim
+    code, tokens, cols, ld = _rows_2d(q, "q")
+    out_code, rows, out_cols, out_ld = _rows_2d(out, "out")
+    if rows != tokens or out_cols != cols or out_code != code:
+        raise ValueError("out must be like q")
+    q_heads = cols // cache.head_dim
+    if q_heads * cache.head_dim != cols:
+        raise ValueError("q must have a column per channel of every head")
     _vector(kv_lens, torch.int32, None, "kv_lens")
     seqs = kv_lens.shape[0]
     _vector(q_offsets, torch.int32, seqs + 1, "q_offsets")
-    _want(page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == seqs
-          and (page_table.stride(1) == 1 or page_table.shape[1] <= 1), "page_table must be int32 [sequences, pages] with contiguous rows")
-    if lse is not None:
-        _want(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (tokens, q_heads), "lse must be contiguous fp32 [tokens, q_heads]")
+    if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.shape[0] != seqs:
+        raise ValueError("page_table must be int32 [sequences, pages]")
+    table_cols = page_table.shape[1]
+    table_stride, step = page_table.stride()
+    if step != 1 and table_cols > 1:
+        raise ValueError("page_table must have contiguous rows")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (tokens, q_heads) or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous fp32 [tokens, q_heads]")
     _here(q, q_offsets, kv_lens, page_table, cache.k, out, lse, workspace)
     _check(lib().vq_attention_paged(q.data_ptr(), code, tokens, ld, q_heads, q_offsets.data_ptr(), kv_lens.data_ptr(), seqs,
-                                    page_table.data_ptr(), max(page_table.stride(0), page_table.shape[1]), page_table.shape[1], cache._ref, float(scale), int(causal),
-                                    int(window), int(max_kv), out.data_ptr(), out_ld, _ptr(lse), _ptr(workspace),
-                                    workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()),
+                                    page_table.data_ptr(), max(table_stride, table_cols), table_cols, cache._ref, scale, causal,
+                                    window, max_kv, out.data_ptr(), out_ld, _ptr(lse), _ptr(workspace),
+                                    0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
            "vq_attention_paged")

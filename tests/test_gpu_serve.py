@@ -510,11 +510,11 @@ def test_layer_of_all(lengths, cache):
     wd = [ref.dequantize(_codes(m), m.scales.cpu(), 128) for m in L.w]
     T = xd.shape[0]
     qkv = (xd @ wd[0].t()).view(T, 12, 64)
-    d = L.desc._keep
+    g_q, g_k, cos, sin = (t.cpu() for t in L.desc._keep)
     at = L.pos.long().cpu()
-    cos, sin = d[4].cpu()[at], d[5].cpu()[at]
-    q, _ = ref.norm_rotate(qkv[:, :8], "rms", d[0].cpu(), None, 1e-6, cos, sin, False)
-    k, _ = ref.norm_rotate(qkv[:, 8:10], "rms", d[2].cpu(), None, 1e-6, cos, sin, False)
+    cos, sin = cos[at], sin[at]
+    q, _ = ref.norm_rotate(qkv[:, :8], "rms", g_q, None, 1e-6, cos, sin, False)
+    k, _ = ref.norm_rotate(qkv[:, 8:10], "rms", g_k, None, 1e-6, cos, sin, False)
     slots = L.slots.cpu()
     k0[slots // 16, :, slots % 16], v0[slots // 16, :, slots % 16] = k, qkv[:, 10:]
     outs, first = [], 0
