@@ -226,13 +226,14 @@ __device__ __forceinline__ void to_lds4(u32 off, const v4i &buf, u32 dst) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" :: "v"(off), "s"(buf), "s"(dst) : "memory");
 }
 
-template <bool WIDE, int WC, int WT, int AT, int TT>
+template <bool WIDE, int WC, int WT, int AT, int TT, int S>
 __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const GemmE4M3Params p) {
     constexpr int kThreads = WC * WT * 64;
     constexpr int TC = WC * AT * 16, TK = WT * TT * 16;              // channels, tokens of the tile
     constexpr int kStage = (TC + TK) * 128 + TK * 4;
     static_assert((TC * 8) % kThreads == 0 && (TK * 8) % kThreads == 0, "a load instruction takes rows of one operand");
     static_assert(TK <= kThreads && TK % 64 == 0, "one scale load per wave");
+    static_assert(S >= 2, "stages");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     // of the weights is channel 32*(r/32) + 8*((r/4)%4) + 4*((r/16)%2) + r%4 of the tile: a lane's results of two channel tiles
     // are then eight consecutive channels.  Rows beyond the matrix and chunks beyond a ragged K arrive as zeros.
     constexpr int kStep = kThreads / 8, kLoadsW = TC / kStep, kLoadsX = TK / kStep;
-    static_assert(TC % kStep == 0 && TK % kStep == 0 && (kStep == 64 || kStep == 32), "rows per load instruction");
+    static_assert(TC % kStep == 0 && TK % kStep == 0 && kStep % 32 == 0, "whole channel groups per load instruction");
     const int r0 = (int)threadIdx.x >> 3;
     const u32 chunk = (u32)((threadIdx.x & 7) ^ (r0 & 7)) * 16u;
     const u32 w_stride = (u32)p.w_stride, x_stride = (u32)p.x_stride;
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     const u32 woff = (u32)(32 * (r0 >> 5) + 8 * ((r0 >> 2) & 3) + 4 * ((r0 >> 4) & 1) + (r0 & 3)) * w_stride + chunk;
     const u32 xoff = (u32)r0 * x_stride + chunk;
 
-    // The stages of all tiles of the workgroup are one sequence; the load cursor runs up to two stages ahead of the sums.
+    // The stages of all tiles of the workgroup are one sequence; the load cursor runs up to S stages ahead of the sums.
     v4i wbuf[kLoadsW], xbuf[kLoadsX];
     uint64_t sbase = 0;
     u32 sbytes = 0;
@@ -294,16 +295,17 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
         sbytes = (u32)rows_x * 4u;
         aim();
     };
-    // part i of the loads of the cursor's stage into buffer `half`; the last part: the tokens' scales
+    // part i of the loads of the cursor's stage into buffer `buf`; the last part: the tokens' scales
     constexpr int kParts = kLoadsW + kLoadsX + 1;
-    auto issue = [&](int half, auto I) {
+    auto issue = [&](int buf, auto I) {
         constexpr int i = decltype(I)::value;
-        const u32 dst = lds0 + (u32)half * kStage + i * (kThreads * 16);
+        const u32 dst = lds0 + (u32)buf * kStage + i * (kThreads * 16);
         if constexpr (i < kLoadsW) to_lds16(w_at, wbuf[i], dst);
         else if constexpr (i < kLoadsW + kLoadsX) to_lds16(x_at, xbuf[i - kLoadsW], dst);
         else {
-            if (wave * 64 < TK)
-                to_lds4(threadIdx.x * 4u, descriptor(sbase, sbytes), lds0 - (u32)wave * 768u + (u32)half * kStage + (TC + TK) * 128);
+            // (every wave, so that all have the same number of loads in flight; beyond the tokens the same ones again)
+            const u32 part = (u32)wave % (TK / 64);
+            to_lds4((part * 64u + (u32)lane) * 4u, descriptor(sbase, sbytes), lds0 - (u32)wave * 1024u + part * 256u + (u32)buf * kStage + (TC + TK) * 128);
             sbase += (uint64_t)p.xs_stride * 4u;
             if (++load_kt == nk) {
                 load_kt = 0;
@@ -317,12 +319,15 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     // The first parts go out when the buffer is free, the others one per channel tile: a burst of all of them queues in the
     // CU's one address path and holds the waves up.
     constexpr int kFirst = kParts - (AT - 2) > 2 ? kParts - (AT - 2) : 2;
+    // Loads retire in order: with the S - 2 younger stages still on their way the oldest one is there.
+    auto landed = []() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"((S - 2) * kParts) : "memory"); };
     point(true);
-    static_for<kParts>([&](auto I) { issue(0, I); });
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int st = 0; st < S - 1; ++st) static_for<kParts>([&](auto I) { issue(st, I); });
+    landed();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    static_for<kFirst>([&](auto I) { issue(1, I); });
+    static_for<kFirst>([&](auto I) { issue(S - 1, I); });
 
     // byte offsets of this lane's two chunks inside a row, and of its rows inside a stage
     const u32 p0 = (u32)((q ^ (l16 & 7)) * 16), p1 = (u32)(((q + 4) ^ (l16 & 7)) * 16);
@@ -344,7 +349,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
         for (int r = 0; r < 4; ++r) acc[i / TT][i % TT][r] = fmaf(d[i % (kLag + 1)][r], sc[i % TT], acc[i / TT][i % TT][r]);
         asm volatile("" : "+v"(acc[i / TT][i % TT]));           // here, not later: the products' registers are needed again
     };
-    int half = 0;
+    int buf = 0;
     for (; id < run1; id += stride) {
     int c0, t0;
     place(id, c0, t0);
@@ -357,8 +362,9 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[a][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     for (int kt = 0; kt < nk; ++kt) {
-        const uint8_t *stage = smem + half * kStage;
-        const uint8_t *next = smem + (half ^ 1) * kStage;
+        const int buf1 = buf + 1 == S ? 0 : buf + 1, behind = buf == 0 ? S - 1 : buf - 1;
+        const uint8_t *stage = smem + buf * kStage;
+        const uint8_t *next = smem + buf1 * kStage;
         const float *xs = reinterpret_cast<const float *>(stage + (TC + TK) * 128) + wt * (16 * TT) + l16;
 #pragma unroll
         for (int t = 0; t < TT; ++t) sc[t] = xs[16 * t] * sw;
@@ -370,15 +376,15 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
             if constexpr (t == 0) {
                 if constexpr (a + 2 < AT) {
                     wf[(a + 2) % 3] = frag(stage, wrow + (a + 2) * 2048);
-                    if constexpr (kFirst + a < kParts) issue(half ^ 1, std::integral_constant<int, kFirst + a>{});
+                    if constexpr (kFirst + a < kParts) issue(behind, std::integral_constant<int, kFirst + a>{});
                 } else if constexpr (a + 1 == AT) {
-                    // every operand of this stage is in registers: its buffer is free once all waves say so, the other is full
-                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                    // every operand of this stage is in registers: its buffer is free once all waves say so, the next is full
+                    landed();
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
                     next0 = frag(next, wrow);
                     next1 = frag(next, wrow + 2048);
-                    static_for<kFirst>([&](auto J) { issue(half, J); });
+                    static_for<kFirst>([&](auto J) { issue(buf, J); });
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -391,7 +397,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
         wf[0] = next0;
         wf[1] = next1;
         static_for<kLag>([&](auto I) { add(AT * TT - kLag + decltype(I)::value); });
-        half ^= 1;
+        buf = buf1;
     }
 
     // a lane's eight consecutive channels of one token per two channel tiles
@@ -423,12 +429,12 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
-template <bool WIDE, int WC, int WT, int AT, int TT>
+template <bool WIDE, int WC, int WT, int AT, int TT, int S>
 hipError_t launch_tile(const GemmE4M3Params &p, hipStream_t stream) {
     constexpr int TC = WC * AT * 16, TK = WT * TT * 16;
-    constexpr int lds = 2 * ((TC + TK) * 128 + TK * 4);
+    constexpr int lds = S * ((TC + TK) * 128 + TK * 4);
     static std::atomic<uint64_t> done{0};
-    auto kern = gemm_e4m3_tile_kernel<WIDE, WC, WT, AT, TT>;
+    auto kern = gemm_e4m3_tile_kernel<WIDE, WC, WT, AT, TT, S>;
     hipError_t e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds, done);
     if (e != hipSuccess) return e;
     const int64_t tiles = (int64_t)((p.Nout + TC - 1) / TC) * ((p.M + TK - 1) / TK);
@@ -438,16 +444,31 @@ hipError_t launch_tile(const GemmE4M3Params &p, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// Which form (us, MI355X, K = 4096 unless given).
+//   Up to 16 tokens: 16 channels a workgroup, so that 256 CUs share 4096 of them (16 x 4096 -> 4096 8.0, 16.8 MB of weights); up to 32:
+//   both token tiles there (9.4, with 32 x 32 blocks 10.8).
+//   Up to 512 blocks of 32 x 32: the waves share K (64 x 4096 -> 4096 11.0, 64 x 128 tiles 21; 256 x 1024 -> 1024 5.7 / 7.9); past
+//   that the operands' second and third reading costs more than LDS (300 x 4096 -> 2000, 630 blocks, 26.9 / 21.8).  Results that cannot
+//   leave in whole stores stay there up to 1000 blocks, more workgroups for the single ones (777 x 1000 -> 1001 7.6 / 9.9).
+//   192 tiles of 256 x 256 and more fill the chip (8192 x 4096 -> 8192 254, with 128 x 128 tiles 337).  fp32 results, whose operands
+//   are widened in registers, do not gain from them (594 against 510).
+//   Up to 256 tiles of 64 x 128: a workgroup per CU, so four stages in its LDS and eight waves, two a SIMD, for one wave a SIMD issues
+//   an instruction every eight to ten cycles (512 x 4096 -> 4096 23.0, four waves 26.3, 128 x 128 on four waves 34).
+//   Else 128 x 128 on eight waves (1024 x 4096 -> 4096 30.2, on four 35.3), fp32 results past a round on four (510 / 541).
 template <bool WIDE>
 hipError_t launch(const GemmE4M3Params &p, hipStream_t stream) {
-    const int64_t blocks = (int64_t)((p.M + 31) / 32) * ((p.Nout + 31) / 32);
+    auto tiles = [&](int tokens, int channels) { return (int64_t)((p.M + tokens - 1) / tokens) * ((p.Nout + channels - 1) / channels); };
     if (p.M <= 16) return launch_split<WIDE, 1, 1, 4>(p, stream);
-    if (blocks <= 1000) return launch_split<WIDE, 2, 2, 1>(p, stream);
+    if (p.M <= 32) return launch_split<WIDE, 1, 2, 2>(p, stream);
+    if (tiles(32, 32) <= (p.vec_ok ? 512 : 1000)) return launch_split<WIDE, 2, 2, 1>(p, stream);
     if constexpr (!WIDE) {
-        const int64_t big = (int64_t)((p.M + 255) / 256) * ((p.Nout + 255) / 256);
-        if (big >= 192) return launch_tile<false, 2, 4, 8, 4>(p, stream);
+        if (tiles(256, 256) >= 192) return launch_tile<false, 2, 4, 8, 4, 2>(p, stream);
     }
-    return launch_tile<WIDE, 2, 2, 4, 4>(p, stream);
+    if (tiles(64, 128) <= 256) return launch_tile<WIDE, 4, 2, 2, 2, 4>(p, stream);
+    if constexpr (WIDE) {
+        if (tiles(128, 128) > 512) return launch_tile<true, 2, 2, 4, 4, 2>(p, stream);
+    }
+    return launch_tile<WIDE, 2, 4, 4, 2, 2>(p, stream);
 }
 
 }  // namespace
