@@ -9,6 +9,7 @@
 
 #include <algorithm>
 
+#include "launch_util.h"
 #include "serve_dev.h"
 
 namespace vitq {
@@ -27,6 +28,22 @@ __device__ __forceinline__ float sum_quarters(float v) {
     v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
     s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// Zeroes the halves of w that are not finite; not 0 if there was one.  (Adding one to an exponent of all ones sets the sign bit
+// alone, and twice a sign bit minus itself shifted to the bottom is a half of ones.)
+template <int DT>
+__device__ __forceinline__ u32 strip(u32 &w) {
+    constexpr u32 kExp = DT == kBF16 ? 0x7F807F80u : 0x7C007C00u, kOne = DT == kBF16 ? 0x00800080u : 0x04000400u;
+    const u32 odd = ((w & kExp) + kOne) & 0x80008000u;
+    w &= ~((odd << 1) - (odd >> 15));
+    return odd;
+}
+// The same for four E4M3 codes, whose one NaN is 0x7F with either sign.
+__device__ __forceinline__ u32 strip_codes(u32 &w) {
+    const u32 odd = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    w &= ~((odd << 1) - (odd >> 7));
+    return odd;
 }
 
 // ---- which rows a workgroup has ------------------------------------------------------------------------------------------
@@ -73,6 +90,27 @@ __device__ __forceinline__ bool find_tile(const PagedParams &p, int tile, RowTil
     return true;
 }
 
+// Infinities and NaN among the values of keys that some rows of a tile see and others do not: zero times them is not zero, so the
+// products of such steps go without them (strip), and where there was one the rows that see its key get it afterwards, here.
+// add(row): the lane's channels of the cache row whose key its row sees.
+template <class F>
+__device__ __forceinline__ void give_back(const PagedParams &p, const int32_t *table, u32 head_unit, int key0, int count, int my_lo, u32 my_span, F &&add) {
+#pragma unroll 1
+    for (int key = key0; key < key0 + count; ++key) {
+        if ((u32)(key - my_lo) >= my_span) continue;
+        const u32 pg = divide((u32)key, p.page_div), page = (u32)table[pg];
+        if (page < p.pages) add(p.v + (uint64_t)(head_unit + page * p.page_units + ((u32)key - pg * p.page_size) * p.token_units) * 16);
+    }
+}
+template <int DT, bool C8>
+__device__ __forceinline__ float odd_value(const uint8_t *row, int c) {       // the channel if it is not finite, or 0
+    if constexpr (C8) return (row[c] & 0x7F) == 0x7F ? __builtin_nanf("") : 0.0f;
+    else {
+        const float v = load1<DT>(row, c);
+        return fabsf(v) < INFINITY ? 0.0f : v;
+    }
+}
+
 // Which tile, head and split a workgroup has.  Workgroups go round-robin to the eight XCDs, each with an L2 of its own.
 // RUNS: one XCD has a run of consecutive tiles of one head and split, which share keys; the last tiles, which see most under a
 // causal mask, start first.  Else splits, then heads, then tiles: evenly spread whatever the lengths (and tiles of one sequence are
@@ -113,13 +151,14 @@ __device__ __forceinline__ void row_range(const PagedParams &p, const RowTile &t
 constexpr int kRows = 16, kStep = 32, kWaves = 4;
 
 template <int DT, bool C8, int DH>
-__global__ __launch_bounds__(kWaves * 64, DH == 64 ? 4 : 2) void paged_rows_kernel(const PagedParams p) {
+__global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) void paged_rows_kernel(const PagedParams p) {
     constexpr int NQ = DH / 32;                               // contraction steps of 32 channels
     constexpr int NT = DH / 16;                               // 16-channel tiles of the output
     constexpr int ND = DH / 32;                               // words of two channels that a lane holds of a V row
     constexpr int KL = C8 ? DH / 64 : DH / 32;                // 16-byte loads of a lane per K tile
     __shared__ __attribute__((aligned(16))) float part[kWaves][kRows][DH + 4];
     __shared__ float part_m[kWaves][kRows], part_l[kWaves][kRows];
+    __shared__ int part_odd[kWaves];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, q4 = lane >> 4;
@@ -161,6 +200,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 4 : 2) void paged_rows_kern
 #pragma unroll
     for (int i = 0; i < NT; ++i) o[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
+    const bool uneven = last_lo > lowest || first_hi < hi;        // the rows do not all see the same keys
+    u32 odd = 0;
 
     // A step's operands as they lie in the cache.  They are requested a step before they are used, and their page numbers a step
     // before that: a wave has one step's keys and values in flight while it works on another's.
@@ -219,6 +260,16 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 4 : 2) void paged_rows_kern
                 s[i] = there && (u32)(first + at) < my_span ? s[i] : -INFINITY;
                 // what is not in the cache must not reach the sums, not even times zero
                 if (!there) x.v[i] = 0;
+            }
+            if (uneven) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int w = 0; w < (C8 ? ND / 2 : ND); ++w) {
+                        u32 v = x.v[i][w];
+                        odd |= C8 ? strip_codes(v) : strip<DT>(v);
+                        x.v[i][w] = v;
+                    }
             }
         }
         float top = s[0];
@@ -285,6 +336,8 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 4 : 2) void paged_rows_kern
         for (int i = 0; i < NT; i += 4)
             *reinterpret_cast<v4f *>(&part[wave][l16][NT * (4 * q4 + rr) + i]) = v4f{o[i][rr], o[i + 1][rr], o[i + 2][rr], o[i + 3][rr]};
     if (q4 == 0) { part_m[wave][l16] = m; part_l[wave][l16] = l; }
+    const bool any_odd = __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+    if (lane == 0) part_odd[wave] = any_odd;
     __syncthreads();
     constexpr int CH = DH / 16;                               // channels per thread: sixteen threads per row
     const int row = threadIdx.x >> 4, c = (threadIdx.x & 15) * CH;
@@ -307,6 +360,14 @@ __global__ __launch_bounds__(kWaves * 64, DH == 64 ? 4 : 2) void paged_rows_kern
 #pragma unroll
     for (int i = 0; i < CH; ++i) y[i] = total == 0.0f ? 0.0f : y[i] * inv;
     const int rr = t.row0 + row;
+    if (part_odd[0] | part_odd[1] | part_odd[2] | part_odd[3]) {
+        int row_lo, row_hi;
+        row_range(p, t, (int)divide(rr, p.group_div), row_lo, row_hi);
+        give_back(p, table, head_unit, lo + step0 * kStep, (step1 - step0) * kStep, row_lo, (u32)(row_hi - row_lo), [&](const uint8_t *v) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) y[i] += odd_value<DT, C8>(v, c + i);
+        });
+    }
     const int token = t.first + (int)divide(rr, p.group_div);
     const int qh = head * p.group + rr - (int)divide(rr, p.group_div) * p.group;
     const int64_t at = (int64_t)token * p.q_heads + qh;
@@ -368,7 +429,8 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
     constexpr int kLoads = kTileKeys / W / kRowsPerLoad;      // per wave, for K and again for V
     constexpr int kTileRows = 32 * W;
     static_assert(kLoads > 0 && kRowsPerLoad <= 16, "every wave loads whole rows");
-    __shared__ __attribute__((aligned(16))) uint8_t smem[4 * kBuf];      // K0 K1 V0 V1
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];       // K0 K1 V0 V1, a flag
+    int *odd = reinterpret_cast<int *>(smem + 4 * kBuf);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h = lane >> 5;
@@ -382,10 +444,10 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
     const int wave_rows = min(32, t.rows - 32 * wave);        // may be <= 0: the wave only helps to load
     const int r = t.row0 + min(32 * wave + l32, t.rows - 1);
     const int tok = (int)divide(r, p.group_div), g = r - tok * p.group;
-    int my_lo, my_hi, lo, hi, x0, x1, w_lo, w_hi, w_first_hi, w_last_lo;
+    int my_lo, my_hi, lo, hi, first_hi, last_lo, w_lo, w_hi, w_first_hi, w_last_lo;
     row_range(p, t, tok, my_lo, my_hi);
-    row_range(p, t, (int)divide(t.row0, p.group_div), lo, x0);
-    row_range(p, t, (int)divide(t.row0 + t.rows - 1, p.group_div), x1, hi);
+    row_range(p, t, (int)divide(t.row0, p.group_div), lo, first_hi);
+    row_range(p, t, (int)divide(t.row0 + t.rows - 1, p.group_div), last_lo, hi);
     {
         const int ra = t.row0 + min(32 * wave, t.rows - 1), rb = t.row0 + min(32 * wave + 31, t.rows - 1);
         row_range(p, t, (int)divide(ra, p.group_div), w_lo, w_first_hi);
@@ -601,6 +663,8 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
         load(unit, ~seen_before == 0, j & 1, V);
         unit = next;
     };
+    const bool uneven = last_lo > lowest || first_hi < hi;               // the rows of the tile do not all see the same keys
+    auto partly = [&](int j) { const int key0 = lo + (step0 + j) * kTileKeys; return key0 < last_lo || key0 + kTileKeys > first_hi; };
     auto arrive = [&](int j) {                                 // ends the half before the products of step j + 1
         if constexpr (C8) {
             if (j + 1 < steps) widen_to_lds((j + 1) & 1, K);
@@ -608,6 +672,20 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        if (uneven && partly(j)) {                            // the wave's own rows of the values
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n)
+#pragma unroll
+                for (int i = 0; i < kRowsPerLoad * RB / 1024; ++i) {
+                    v4u *at = reinterpret_cast<v4u *>(smem + (2 + (j & 1)) * kBuf + (kNext * n + wave * kRowsPerLoad) * RB + i * 1024 + lane * 16);
+                    v4u w = *at;
+                    u32 found = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { u32 x = w[e]; found |= strip<DT>(x); w[e] = x; }
+                    if (found != 0) { *at = w; *odd = 1; }
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
     };
     auto barrier = [&]() {
@@ -619,6 +697,7 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
     };
     const std::integral_constant<bool, true> yes;
     const std::integral_constant<bool, false> no;
+    if (threadIdx.x == 0) *odd = 0;                           // (the first barrier is ahead of its first use)
     if (steps > 0) {
         ask(step0);
         unit = answer();
@@ -667,6 +746,20 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
             arrive(steps - 1);
             barrier();
             if (works) products(yes, no, smem + (2 + ((steps - 1) & 1)) * kBuf, nullptr);
+        }
+        if (uneven && works && *odd) {
+            for (int j = 0; j < steps; ++j) {
+                if (!partly(j)) continue;
+                give_back(p, table, head_unit, lo + (step0 + j) * kTileKeys, kTileKeys, my_lo, my_span, [&](const uint8_t *row) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            o[d][i] += odd_value<DT, C8>(row, 32 * d + 8 * (i >> 2) + 4 * h + (i & 3));
+                            __builtin_amdgcn_sched_barrier(0);  // (rare: registers count, not time)
+                        }
+                });
+            }
         }
     }
     {
@@ -809,7 +902,12 @@ hipError_t launch(PagedParams &p, hipStream_t stream) {
     hipError_t e = hipSuccess;
     if (f.many) {
         p.row_tiles = (int)(p.tokens * p.group / kWgRows) + p.seqs;
-        hipLaunchKernelGGL((paged_tiles_kernel<DT, C8, DH, kWgRows / 32>), dim3((u32)((int64_t)p.row_tiles * p.kv_heads * p.splits)), dim3(2 * kWgRows), 0, stream, p);
+        auto kern = paged_tiles_kernel<DT, C8, DH, kWgRows / 32>;
+        constexpr int lds = 4 * 64 * DH * 2 + 16;
+        static std::atomic<uint64_t> done{0};
+        e = allow_dynamic_lds(reinterpret_cast<const void *>(kern), lds, done);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3((u32)((int64_t)p.row_tiles * p.kv_heads * p.splits)), dim3(2 * kWgRows), lds, stream, p);
         e = hipGetLastError();
     }
     if (e == hipSuccess && f.few) {

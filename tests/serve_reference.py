@@ -117,7 +117,12 @@ def attention(q, keys, values, place, scale, causal, window, kv_len, visible=Non
         if not bool(some.any()):
             continue
         p = torch.softmax(z[some], dim=1)
-        out[some, h] = p @ v
+        fine = torch.isfinite(v)
+        out[some, h] = p @ torch.where(fine, v, torch.zeros_like(v))
+        for key in torch.nonzero(~fine.all(1)).flatten().tolist():        # what is not finite reaches the rows that see its key alone
+            rows = torch.nonzero(some & seen[:, key]).flatten()
+            out[rows, h] = out[rows, h] + torch.where(fine[key], torch.zeros_like(v[key]), v[key])
+        v = torch.where(fine, v, torch.zeros_like(v))
         lse[some, h] = torch.logsumexp(z[some], dim=1)
         mass[some, h] = p @ v.abs()
         reach[some, h] = torch.where(seen, (q[:, h].abs() @ k.abs().t()) * abs(scale), torch.zeros_like(z))[some].max(1).values
