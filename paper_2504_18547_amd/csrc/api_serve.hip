@@ -209,7 +209,9 @@ vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64
     if (((uintptr_t)q_offsets | (uintptr_t)kv_lens | (uintptr_t)page_table | (uintptr_t)lse) % 4 != 0) return VQ_ERR_STRIDE;
     // an `out` that overlaps q must be q: the rows are read and written by the same workgroup
     if (q == out && q_ld != out_ld) return VQ_ERR_STRIDE;
-    if (max_kv == 0) max_kv = (int64_t)table_cols * cache->page_size;
+    const int64_t most = (int64_t)table_cols * cache->page_size;
+    if (max_kv == 0 || max_kv > most) max_kv = most;
+    if (window > (1 << 30)) window = 0;                       // reaches past every first key
     // (a window shortens what a tile of rows sees; the workspace, which knows of none, is then more than enough)
     const int64_t longest = window > 0 && window + 256 < max_kv ? window + 256 : max_kv;
     vitq::PagedParams p{};

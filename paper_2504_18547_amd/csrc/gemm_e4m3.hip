@@ -200,9 +200,13 @@ hipError_t launch_split(const GemmE4M3Params &p, hipStream_t stream) {
 
 // ---- many tiles: operands through LDS ------------------------------------------------------------------------------------
 // A workgroup of WC x WT waves owns WC*AT*16 channels x WT*TT*16 tokens; a stage is one block of the contraction (128 bytes of
-// every row and the tokens' scales), two stages in LDS, filled by loads that go straight there.  LDS rows are unpadded, their
+// every row and the tokens' scales), S stages in LDS, filled by loads that go straight there.  LDS rows are unpadded, their
 // 16-byte chunks permuted by the row so that the sixteen rows of an operand spread over the banks; weight rows sit in an order
-// that gives a lane sixteen consecutive channels over four channel tiles.
+// that gives a lane eight consecutive channels over two channel tiles.
+// 8192 x 4096 -> 8192: 254-260 us, 2.1 PFLOP/s; with one scale a tensor a library product reaches 3.2 on this card.  The matrix cores
+// are busy 51 % of the time.  Without the FMAs that scale each block's products into the totals it took 27 us less, without the loads
+// to LDS 43, without the stores 34: they add up, for a SIMD's two waves issue little more than an instruction every four cycles.
+// Left out: products of the next stage's loads all at once (254 as well), 16 waves (registers spill).
 __device__ __forceinline__ u32 lds_address_of(const void *p) {
     return (u32)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p;
 }

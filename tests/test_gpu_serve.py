@@ -479,6 +479,32 @@ def test_attention_rows_outside_every_sequence_and_cut_lengths():
     assert torch.equal(o3, o4)
 
 
+def test_attention_hints_and_windows_past_every_length():
+    _check_attention([(1, 300), (8, 3), (70, 90)], 4, 2, 64, BF16, causal=False, window=2 ** 31 - 1, max_kv=2 ** 40)
+    _check_attention([(1, 300), (8, 3), (70, 90)], 4, 2, 64, BF16, window=2 ** 31 - 1)
+    args, out, _ = _check_attention([(1, 300), (8, 3), (70, 90)], 4, 2, 64, BF16)
+    empty = args[3][:, :0].contiguous()                               # a table without columns: nobody sees anything
+    o, lse = torch.empty_like(out), torch.empty(79, 4, device="cuda")
+    vitq.vq_attention_paged(*args[:3], empty, *args[4:], o, lse, None)
+    assert not bool(o.any()) and bool((lse == -math.inf).all())
+
+
+def test_tensors_elsewhere_are_refused():
+    m = vitq.FMat.empty(4, 128)
+    with pytest.raises(ValueError):
+        vitq.vq_quantize_e4m3(torch.zeros(4, 128), m)
+    with pytest.raises(ValueError):
+        vitq.vq_quantize_e4m3(torch.zeros(4, 128, device="cuda"), vitq.FMat.empty(4, 128, device="cpu"))
+    args, out, _ = _check_attention([(1, 30)], 4, 2, 64, BF16)
+    with pytest.raises(ValueError):
+        vitq.vq_attention_paged(*args[:2], args[2].cpu(), *args[3:], out, None, None)
+    with pytest.raises(ValueError):
+        vitq.vq_attention_paged(*args[:2], args[2].long(), *args[3:], out, None, None)
+    with pytest.raises(vitq.VitqError):                               # more splits than the workspace has room for
+        long = torch.zeros(1, 4096, dtype=torch.int32, device="cuda")
+        vitq.vq_attention_paged(args[0], args[1], args[2], long, args[4], 0.1, True, 0, 65536, out, None, torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
 def test_attention_in_place():
     args, out, _ = _check_attention([(3, 40), (70, 300), (1, 1200)], 4, 2, 64, F16)
     q = args[0].clone()

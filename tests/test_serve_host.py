@@ -145,7 +145,8 @@ def test_rotate_arguments(lib, change, status):
     (dict(tokens=-1), "ERR_SHAPE"), (dict(seqs=-1), "ERR_SHAPE"), (dict(tokens=1 << 23), "ERR_SHAPE"), (dict(q_ld=252), "ERR_STRIDE"),
     (dict(out_ld=260), "ERR_STRIDE"), (dict(q=P + 2), "ERR_STRIDE"), (dict(ts=3), "ERR_STRIDE"), (dict(window=-1), "ERR_SHAPE"),
     (dict(tc=1 << 28, ts=1 << 28), "ERR_SHAPE"), (dict(scale=float("nan")), "ERR_STEP"), (dict(max_kv=-1), "ERR_SHAPE"),
-    (dict(max_kv=100000), "ERR_WORKSPACE"), (dict(max_kv=100000, ws=P, wb=16), "ERR_WORKSPACE"), (dict(max_kv=100000, ws=P + 4, wb=1 << 40), "ERR_STRIDE"),
+    (dict(max_kv=0, tc=8192, ts=8192), "ERR_WORKSPACE"), (dict(max_kv=100000, tc=8192, ts=8192, ws=P, wb=16), "ERR_WORKSPACE"),
+    (dict(max_kv=100000, tc=8192, ts=8192, ws=P + 4, wb=1 << 40), "ERR_STRIDE"),
     (dict(lens=P + 2), "ERR_STRIDE"), (dict(out_ld=264), "ERR_STRIDE"), (dict(tokens=0), "OK"), (dict(seqs=0), "OK")])
 def test_attention_arguments(lib, change, status):
     assert _attend(lib, **change) == E[status]
