@@ -150,6 +150,8 @@ __device__ __forceinline__ void row_range(const PagedParams &p, const RowTile &t
 // of O^T: operand t has channel 8m + t in row m.  Nothing passes through LDS until the waves' results are joined.
 // Bound by HBM: 64 x 8,192 keys of 8 heads of 128 in bf16 362-367 us, 5.9 TB/s; in E4M3 with lengths of 1 to 8,192 122 us, 4.6 TB/s
 // (the widening and the unequal lengths); a step's operands requested while the step before is worked on took 10 % off both.
+// Waves a SIMD: as many as the registers give without spills.  64 channels of 16 bits forced to four spill 20-92 bytes: single tokens,
+// 64 x 4,096 keys of 4 heads, 66-77 us against 61; a chunk of 511 rows among single tokens 48-67 against 50.
 constexpr int kRows = 16, kStep = 32, kWaves = 4;
 
 template <int DT, bool C8, int DH>
@@ -398,8 +400,8 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
 // transposing LDS read, four keys of one channel per lane, in the order in which the score registers hold the keys; B = P^T.
 // LDS rows are unpadded with their 16-byte chunks permuted by the row: K's so that 16 rows' equal chunks cover all banks, V's so
 // that four rows' 64-byte pieces do.
-// 2 x 2,048 tokens over 8,192 keys, 32 / 8 heads of 128: 417-437 us, 1.10-1.15 PFLOP/s of the 1.43 that a large bf16 library product
-// reaches on this card; the matrix cores are busy 57 % of the time, the rest goes to the issue of what stands between their
+// 2 x 2,048 tokens over 8,192 keys, 32 / 8 heads of 128: 449-456 us, 1.06-1.07 PFLOP/s of the 1.43 that a large bf16 library product
+// reaches on this card (3 % of the time keeps infinities and NaN from rows that do not see their keys); the matrix cores are busy 57 % of the time, the rest goes to the issue of what stands between their
 // instructions (no loads: 391, no exponentials: 410).  Left out: steps of 32 keys (535), with them three waves a SIMD (535), the
 // exponentials of one step among the score products of the next in one wave (504, registers spill).
 
@@ -703,7 +705,7 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
     };
     const std::integral_constant<bool, true> yes;
     const std::integral_constant<bool, false> no;
-    if (threadIdx.x == 0) *odd = 0;                           // (the first barrier is ahead of its first use)
+    if (threadIdx.x == 0) *odd = 0;                           // (waited for before the first barrier, which is ahead of its first use)
     if (steps > 0) {
         ask(step0);
         unit = answer();
@@ -714,7 +716,7 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
             widen_to_lds(0, K);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // the keys, and the flag's zero
         }
         barrier();
         if (second) {
