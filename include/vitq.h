@@ -453,8 +453,8 @@ typedef struct vq_kv_cache {
  * (i, i + rot_dim/2), or (2i, 2i+1) if interleaved.  Any rotation is one of its tables: two-dimensional
  * positions of image tokens are a table with one row per place.  All in fp32, rounded once.
  * gamma / beta: device fp32 [head_dim] for all heads (gamma_head_stride 0) or one row per head
- * (gamma_head_stride >= head_dim, elements, a multiple of 4); beta nullable.  gamma, beta and the
- * tables are 16-byte aligned.
+ * (gamma_head_stride >= head_dim, elements, a multiple of 4); beta nullable; a call that does not want
+ * queries (keys and values) needs no q_gamma (k_gamma).  gamma, beta and the tables are 16-byte aligned.
  */
 typedef struct vq_rotate_desc {
     int32_t q_heads, kv_heads, head_dim;

@@ -162,6 +162,8 @@ vq_status vq_qkv_norm_rotate(const vq_rotate_desc *d, const void *qkv, int32_t d
     vitq::RotateParams p{};
     p.qkv = qkv; p.ld = ld; p.tokens = tokens;
     p.q_heads = d->q_heads; p.kv_heads = d->kv_heads; p.head_dim = d->head_dim;
+    p.head_begin = q_out ? 0 : d->q_heads;
+    p.head_end = cache ? d->q_heads + 2 * d->kv_heads : d->q_heads;
     p.norm = d->norm; p.rot_dim = d->rot_dim; p.interleaved = d->interleaved ? 1 : 0;
     p.q_gamma = d->q_gamma; p.q_beta = d->q_beta; p.k_gamma = d->k_gamma; p.k_beta = d->k_beta;
     p.gamma_stride = d->gamma_head_stride;

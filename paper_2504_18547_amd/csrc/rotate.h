@@ -10,6 +10,7 @@ namespace vitq {
 struct RotateParams {
     const void *qkv; int64_t ld; int64_t tokens;
     int q_heads, kv_heads, head_dim;
+    int head_begin, head_end;                          // heads of a row (queries, keys, values) whose outputs are wanted
     int norm, rot_dim, interleaved;
     const float *q_gamma, *q_beta, *k_gamma, *k_beta; int64_t gamma_stride;
     const float *cos_table, *sin_table; int64_t table_rows;

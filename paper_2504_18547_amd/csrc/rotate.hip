@@ -6,7 +6,8 @@
 // A group of L lanes (the power of two with 8 L >= head_dim) owns one head of one token, eight channels per lane: loads and
 // stores of 16 bytes per lane are whole rows of a head, the statistics are sums over the group, and the rotation's partner
 // channels (rot_dim/2 further) are eight channels of one other lane.  A workgroup takes 256 / L x ITER heads of one token, so the
-// token's angles are read once for ITER heads.
+// token's angles are read once for ITER heads.  The heads are those whose outputs are wanted: of the others neither values nor
+// gammas are read (there may be none).
 #include "rotate.h"
 #include "serve_dev.h"
 
@@ -47,8 +48,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateParams p) {
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     const int c0 = 8 * lane;
     const bool live = c0 < p.head_dim;
-    const int heads = p.q_heads + 2 * p.kv_heads;
-    const int h0 = blockIdx.y * (kGroups * ITER) + group;
+    const int heads = p.head_end;
+    const int h0 = p.head_begin + blockIdx.y * (kGroups * ITER) + group;
 
     float c[8], s[8];
     const int half = p.rot_dim >> 1;
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateParams p) {
         }
         if (mine) {
             if (is_q) {
-                if (p.q_out) store_channels((uint8_t *)p.q_out, t * p.q_ld + (int64_t)h * p.head_dim + c0, p.q_dtype, v, 1.0f);
+                store_channels((uint8_t *)p.q_out, t * p.q_ld + (int64_t)h * p.head_dim + c0, p.q_dtype, v, 1.0f);
             } else if (row >= 0) {
                 const int hh = is_v ? hk - p.kv_heads : hk;
                 store_channels(is_v ? p.v : p.k, row + hh * p.head_stride + c0, p.cache_dtype, v, is_v ? p.v_inv : p.k_inv);
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(const RotateParams p) {
 template <int DT, int L>
 hipError_t launch(const RotateParams &p, hipStream_t stream) {
     constexpr int kGroups = 256 / L;
-    const int heads = p.q_heads + 2 * p.kv_heads;
+    const int heads = p.head_end - p.head_begin;
     const int rounds = (heads + kGroups - 1) / kGroups;
     // few tokens: every round of heads is a workgroup of its own (one token: 7.4 us a call, nearly all of it the host's)
     if (p.tokens * rounds <= 2048 || rounds == 1) {

@@ -1,0 +1,36 @@
+"""Serving-layer operators on the GPU: calls at the edges of what their documentation allows."""
+import pytest
+import torch
+
+from paper_2504_18547_amd import vitq
+from tests.test_gpu_serve import BF16, _gen
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- norm + rotation + append ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("T,Hq,Hk,D", [(1, 4, 2, 64), (33, 7, 1, 128), (900, 32, 8, 128), (5, 2, 2, 256), (3, 1, 1, 24)])
+def test_rotate_one_output_without_the_others_gamma(T, Hq, Hk, D, norm):
+    """Queries alone need no gamma for the keys, keys and values alone none for the queries; the bits are those of the full call."""
+    g = _gen(T + D)
+    qkv = torch.randn(T, (Hq + 2 * Hk) * D, generator=g).to(BF16).cuda()
+    angle = torch.rand(64, D // 16 * 8, generator=g) * 6.3
+    cos, sin = angle.cos().cuda(), angle.sin().cuda()
+    pos = torch.randint(0, 64, (T,), generator=g).int().cuda()
+    slots = torch.randperm(T + 20, generator=g)[:T].cuda()
+    gq, gk = [(1 + 0.2 * torch.randn(D, generator=g)).cuda() for _ in range(2)]
+    bq, bk = [(0.1 * torch.randn(D, generator=g)).cuda() if norm == "layer" else None for _ in range(2)]
+    pages = -(-(T + 20) // 16)
+
+    def call(desc, want_q, want_kv):
+        q = torch.full((T, Hq * D), 5.0, dtype=BF16, device="cuda")
+        c = vitq.KvCache(*[torch.full((pages, Hk, 16, D), 5.0, dtype=BF16, device="cuda") for _ in range(2)])
+        vitq.vq_qkv_norm_rotate(desc, qkv, pos, q if want_q else None, c if want_kv else None, slots if want_kv else None)
+        return q, c.k, c.v
+    full = call(vitq.make_rotate_desc(Hq, Hk, D, norm, gq, bq, gk, bk, 1e-6, cos, sin), True, True)
+    q, k, v = call(vitq.make_rotate_desc(Hq, Hk, D, norm, gq, bq, None, None, 1e-6, cos, sin), True, False)
+    assert torch.equal(q, full[0]) and bool((k == 5.0).all()) and bool((v == 5.0).all())
+    q, k, v = call(vitq.make_rotate_desc(Hq, Hk, D, norm, None, None, gk, bk, 1e-6, cos, sin), False, True)
+    assert bool((q == 5.0).all()) and torch.equal(k, full[1]) and torch.equal(v, full[2])
