@@ -578,7 +578,7 @@ def vq_attention_paged(q, q_offsets, kv_lens, page_table, cache, scale, causal, 
         raise ValueError("lse must be contiguous fp32 [tokens, q_heads]")
     _here(q, q_offsets, kv_lens, page_table, cache.k, out, lse, workspace)
     _check(lib().vq_attention_paged(q.data_ptr(), code, tokens, ld, q_heads, q_offsets.data_ptr(), kv_lens.data_ptr(), seqs,
-                                    page_table.data_ptr(), max(table_stride, table_cols), table_cols, cache._ref, scale, causal,
+                                    page_table.data_ptr(), table_stride if seqs > 1 else table_cols, table_cols, cache._ref, scale, causal,
                                     window, max_kv, out.data_ptr(), out_ld, _ptr(lse), _ptr(workspace),
                                     0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
            "vq_attention_paged")
