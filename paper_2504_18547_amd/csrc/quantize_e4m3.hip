@@ -28,10 +28,17 @@ __device__ __forceinline__ void gather8(const QuantE4M3Params &p, int64_t r, int
     for (int i = 0; i < 8; ++i) v[i] = (r < p.rows && c + i < p.cols) ? load1<DT>(p.x, r * p.ld + c + i) : 0.0f;
 }
 
-__device__ __forceinline__ void store8(const QuantE4M3Params &p, int64_t r, int64_t c, const float (&v)[8], float f) {
+// The bytes of the eight columns c.. that are the matrix's own: a row's padding is written as zero, beside a NaN too (where zero
+// times the factor is not).
+__device__ __forceinline__ uint2 own_bytes(const QuantE4M3Params &p, int64_t c) {
+    const int valid = (int)min(p.cols - c, (int64_t)8);
+    const uint64_t keep = valid > 0 ? ~uint64_t(0) >> (64 - 8 * valid) : 0;
+    return make_uint2((u32)keep, (u32)(keep >> 32));
+}
+__device__ __forceinline__ void store8(const QuantE4M3Params &p, int64_t r, int64_t c, const float (&v)[8], float f, uint2 keep) {
     uint2 w;
-    w.x = pack_e4m3(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-    w.y = pack_e4m3(v[4] * f, v[5] * f, v[6] * f, v[7] * f);
+    w.x = pack_e4m3(v[0] * f, v[1] * f, v[2] * f, v[3] * f) & keep.x;
+    w.y = pack_e4m3(v[4] * f, v[5] * f, v[6] * f, v[7] * f) & keep.y;
     *reinterpret_cast<uint2 *>(p.codes + r * p.code_stride + c) = w;
 }
 
@@ -61,7 +68,7 @@ __global__ __launch_bounds__(256) void quantize_e4m3_rows_kernel(const QuantE4M3
         const u32 m = reduce_lanes(max_bits(v[u]), 16, [](u32 a, u32 b) { return max(a, b); });
         const float a = __uint_as_float(max(m, __float_as_uint(kTiny)));
         if (r < p.rows && c < padded) {
-            store8(p, r, c, v[u], kMaxE4M3 / a);
+            store8(p, r, c, v[u], kMaxE4M3 / a, own_bytes(p, c));
             if (lane16 == 0) p.scales[(c >> 7) * p.scale_stride + r] = a / kMaxE4M3;
         }
     }
@@ -104,13 +111,14 @@ __global__ __launch_bounds__(256) void quantize_e4m3_blocks_kernel(const QuantE4
     const float f = kMaxE4M3 / a;
     if (threadIdx.x == 0) p.scales[(int64_t)blockIdx.y * p.scale_stride + blockIdx.x] = a / kMaxE4M3;
     if (c >= padded) return;
+    const uint2 keep = own_bytes(p, c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t r = r0 + row0 + 16 * i;
         if (r >= p.rows) continue;
         if (vec) values8<DT>(raw[i], v);
         else gather8<DT>(p, r, c, v);
-        store8(p, r, c, v, f);
+        store8(p, r, c, v, f, keep);
     }
 }
 

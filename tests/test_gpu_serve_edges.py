@@ -1,9 +1,11 @@
 """Serving-layer operators on the GPU: calls at the edges of what their documentation allows."""
+import math
+
 import pytest
 import torch
 
 from paper_2504_18547_amd import vitq
-from tests.test_gpu_serve import BF16, _gen
+from tests.test_gpu_serve import BF16, F16, F32, _codes, _gen
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +36,25 @@ def test_rotate_one_output_without_the_others_gamma(T, Hq, Hk, D, norm):
     assert torch.equal(q, full[0]) and bool((k == 5.0).all()) and bool((v == 5.0).all())
     q, k, v = call(vitq.make_rotate_desc(Hq, Hk, D, norm, None, None, gk, bk, 1e-6, cos, sin), False, True)
     assert bool((q == 5.0).all()) and torch.equal(k, full[1]) and torch.equal(v, full[2])
+
+
+# ---- quantizer ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (20, 200), (130, 129), (5, 1001)])
+def test_quantize_padding_beside_what_is_not_finite(rows, cols, dtype, block_rows):
+    """The bytes behind the last column are zero also where the block's scale is NaN or infinite."""
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        x = torch.randn(rows, cols, generator=_gen(rows + cols)).to(dtype)
+        x[rows // 2, cols - 1] = bad
+        m = vitq.FMat.empty(rows, cols, block_rows)
+        m.data.fill_(0xA5)
+        vitq.vq_quantize_e4m3(x.cuda(), m)
+        assert not bool(m.data[:, cols:].any()), bad
+        codes = _codes(m)
+        last = codes[rows // 2 // block_rows * block_rows:(rows // 2 // block_rows + 1) * block_rows, (cols - 1) // 128 * 128:]
+        if math.isnan(bad):
+            assert bool(torch.isnan(last).all())
+        else:
+            assert math.isnan(float(codes[rows // 2, cols - 1])) and int(torch.isnan(last).sum()) == 1
