@@ -39,7 +39,7 @@ __device__ __forceinline__ void store4(const GemmE4M3Params &p, int m, int n, v4
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if (p.bias && r < valid) y[r] += p.bias[n + r];
-        if (p.act) y[r] = gelu_fast(y[r]);
+        if (p.act) y[r] = gelu_any(y[r]);
     }
     const int64_t at = (int64_t)m * p.ld + n;
     if (p.y_dtype == kF32) {
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(WC *WT * 64, 2) void gemm_e4m3_tile_kernel(const Ge
             for (int j = 0; j < 8; ++j) y[j] = acc[2 * g + (j >> 2)][t][j & 3] + b[j];
             if (p.act) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = gelu_fast(y[j]);
+                for (int j = 0; j < 8; ++j) y[j] = gelu_any(y[j]);
             }
             if (m < p.M) {
                 if constexpr (WIDE) store8_f32(p, m, n, y, full);

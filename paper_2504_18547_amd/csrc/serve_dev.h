@@ -67,6 +67,12 @@ __device__ __forceinline__ v4u widen8(u32 lo, u32 hi) {
     return r;
 }
 
+// 0.5 y (1 + tanh(..)) for any y: gelu_fast is for finite ones, and at +infinity takes infinity times zero from infinity.
+__device__ __forceinline__ float gelu_any(float y) {
+    const float g = gelu_fast(y);
+    return y == INFINITY ? y : g;
+}
+
 // One element of any of the three input types.
 template <int DT>
 __device__ __forceinline__ float load1(const void *p, int64_t i) {

@@ -58,3 +58,31 @@ def test_quantize_padding_beside_what_is_not_finite(rows, cols, dtype, block_row
             assert bool(torch.isnan(last).all())
         else:
             assert math.isnan(float(codes[rows // 2, cols - 1])) and int(torch.isnan(last).sum()) == 1
+
+
+# ---- linear -----------------------------------------------------------------------------------------------------
+
+def _random_fmats(M, K, N, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    xm, wm = vitq.FMat.empty(M, K, 1), vitq.FMat.empty(N, K, 128)
+    vitq.vq_quantize_e4m3(torch.randn(M, K, generator=g, device="cuda"), xm)
+    vitq.vq_quantize_e4m3(torch.randn(N, K, generator=g, device="cuda") * 0.05, wm)
+    return xm, wm
+
+
+# blocks of 16 and of 32 channels with K shared by the waves, then tiles of 64 x 128, 128 x 128 and 256 x 256 (fp32: 128 x 128)
+@pytest.mark.parametrize("out", [F32, BF16, F16])
+@pytest.mark.parametrize("M,K,N", [(5, 200, 48), (24, 200, 64), (60, 200, 130), (520, 129, 2050), (1025, 129, 4100), (4100, 129, 4112)])
+def test_linear_gelu_of_infinite_sums(M, K, N, out):
+    """0.5 y (1 + tanh(..)) is +infinity at +infinity, and NaN (0 times infinity) at -infinity."""
+    xm, wm = _random_fmats(M, K, N, M + N)
+    plain, y = (torch.empty(M, N, dtype=out, device="cuda") for _ in range(2))
+    bias = torch.zeros(N, device="cuda")
+    vitq.vq_linear_e4m3(xm, wm, bias, 1, plain)
+    at = torch.tensor([0, 7, N - 1]).cuda()
+    bias[at] = float("inf")
+    bias[9] = float("-inf")
+    vitq.vq_linear_e4m3(xm, wm, bias, 1, y)
+    assert bool((y[:, at] == math.inf).all()) and bool(torch.isnan(y[:, 9]).all())
+    rest = bias == 0
+    assert bool(torch.isfinite(plain).all()) and torch.equal(y[:, rest], plain[:, rest])
