@@ -419,7 +419,7 @@ vq_status vq_quantize_e4m3(const void *x, int32_t x_dtype, int64_t rows, int64_t
  * x: [M x K], block_rows 1; w: [Nout x K], block_rows 128 (else UNSUPPORTED).  bias: device fp32
  * [Nout] or NULL.  act: 0 none, 1 GELU (tanh form).  y: device [M x Nout], leading dimension ld
  * (elements), aligned to its type.  Limits: K <= 65536, row strides of both operands below 2^24 bytes.
- * The order of the sums depends on the sizes alone: equal calls give equal bits.
+ * The order of the sums depends on the sizes and y_dtype alone: equal products give equal bits, wherever they go.
  * Errors: NULL, SHAPE, BITS (y_dtype), STRIDE, UNSUPPORTED.
  */
 vq_status vq_linear_e4m3(const vq_fmat *x, const vq_fmat *w, const float *bias, int32_t act, void *y,

@@ -452,8 +452,12 @@ hipError_t launch_tile(const GemmE4M3Params &p, hipStream_t stream) {
 //   Up to 16 tokens: 16 channels a workgroup, so that 256 CUs share 4096 of them (16 x 4096 -> 4096 8.0, 16.8 MB of weights); up to 32:
 //   both token tiles there (9.4, with 32 x 32 blocks 10.8).
 //   Up to 512 blocks of 32 x 32: the waves share K (64 x 4096 -> 4096 11.0, 64 x 128 tiles 21; 256 x 1024 -> 1024 5.7 / 7.9); past
-//   that the operands' second and third reading costs more than LDS (300 x 4096 -> 2000, 630 blocks, 26.9 / 21.8).  Results that cannot
-//   leave in whole stores stay there up to 1000 blocks, more workgroups for the single ones (777 x 1000 -> 1001 7.6 / 9.9).
+//   that the operands' second and third reading costs more than LDS (300 x 4096 -> 2000, 630 blocks, 26.4 / 18.8), the sooner where
+//   rows are a multiple of 128 bytes and start in the same memory channels.  fp32 results, which are bound by the widening, stay up to
+//   768, three workgroups a CU (760 x 4096 -> 1000 26.3 / 28.9; 777 x 4096 -> 1000, 800 blocks, 32.0 / 28.6).  Up to 1000 blocks of a short K: fp32
+//   (777 x 1000 -> 1000 7.6 / 10.9, K 1024 10.8 / 10.8, K 1536 15.5 / 13.8); 16 bits where K is ragged (7.2 / 8.0, K 896 9.7 / 7.6,
+//   K 1536 13.7 / 9.5) or the channels are, whose results leave as single stores (777 x 1000 -> 1001 7.5 / 10.2, 540 x 896 -> 1001
+//   8.2 / 9.5).  The rule looks at sizes alone, not at where the results go, so that equal products have equal bits.
 //   192 tiles of 256 x 256 and more fill the chip (8192 x 4096 -> 8192 254, with 128 x 128 tiles 337).  fp32 results, whose operands
 //   are widened in registers, do not gain from them (594 against 510).
 //   Up to 256 tiles of 64 x 128: a workgroup per CU, so four stages in its LDS and eight waves, two a SIMD, for one wave a SIMD issues
@@ -464,7 +468,9 @@ hipError_t launch(const GemmE4M3Params &p, hipStream_t stream) {
     auto tiles = [&](int tokens, int channels) { return (int64_t)((p.M + tokens - 1) / tokens) * ((p.Nout + channels - 1) / channels); };
     if (p.M <= 16) return launch_split<WIDE, 1, 1, 4>(p, stream);
     if (p.M <= 32) return launch_split<WIDE, 1, 2, 2>(p, stream);
-    if (tiles(32, 32) <= (p.vec_ok ? 512 : 1000)) return launch_split<WIDE, 2, 2, 1>(p, stream);
+    const int64_t blocks = tiles(32, 32);
+    const bool short_k = WIDE ? p.K <= 1024 : p.K <= 1000 && (p.K % 128 != 0 || p.Nout % 8 != 0);
+    if (blocks <= (WIDE ? 768 : 512) || (blocks <= 1000 && short_k)) return launch_split<WIDE, 2, 2, 1>(p, stream);
     if constexpr (!WIDE) {
         if (tiles(256, 256) >= 192) return launch_tile<false, 2, 4, 8, 4, 2>(p, stream);
     }

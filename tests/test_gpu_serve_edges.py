@@ -86,3 +86,15 @@ def test_linear_gelu_of_infinite_sums(M, K, N, out):
     assert bool((y[:, at] == math.inf).all()) and bool(torch.isnan(y[:, 9]).all())
     rest = bias == 0
     assert bool(torch.isfinite(plain).all()) and torch.equal(y[:, rest], plain[:, rest])
+
+
+@pytest.mark.parametrize("out", [F32, BF16, F16])
+@pytest.mark.parametrize("M,K,N", [(777, 1000, 1000), (520, 640, 1920), (200, 1000, 2999), (3000, 300, 160), (777, 300, 1001), (300, 129, 2050)])
+def test_linear_sums_do_not_depend_on_where_results_go(M, K, N, out):
+    xm, wm = _random_fmats(M, K, N, M * N)
+    ref_y = torch.empty(M, (N + 15) // 16 * 16, dtype=out, device="cuda")[:, :N]
+    vitq.vq_linear_e4m3(xm, wm, None, 0, ref_y)
+    for pad, first in ((1, 0), (3, 1), (16, 8), (8, 4)):
+        y = torch.empty(M, (N + 15) // 16 * 16 + pad + 8, dtype=out, device="cuda")[:, first:first + N]
+        vitq.vq_linear_e4m3(xm, wm, None, 0, y)
+        assert torch.equal(y, ref_y), (pad, first)
