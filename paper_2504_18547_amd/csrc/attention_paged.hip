@@ -30,6 +30,15 @@ __device__ __forceinline__ float sum_quarters(float v) {
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// Probabilities are exp2(score - base), and in half precision base lies this far below the largest score (in powers of two): what is
+// far below the largest keeps 2^-39 of it (rows kernel; 2^-31 at least in the tiles kernel, whose base lags) instead of 2^-24, which
+// counts where many such keys stand beside a strong one.  The sums carry the same factor, so it falls out by itself.
+template <int DT>
+constexpr float kLiftRows = DT == kF16 ? 15.0f : 0.0f;        // 2^15: half precision ends at 65504
+constexpr float kLag = 8.0f;                                  // by how much a row's largest score may pass base + lift in the tiles kernel
+template <int DT>
+constexpr float kLiftTiles = DT == kF16 ? 15.0f - kLag : 0.0f;
+
 // Zeroes the halves of w that are not finite; not 0 if there was one.  (Adding one to an exponent of all ones sets the sign bit
 // alone, and twice a sign bit minus itself shifted to the bottom is a half of ones.)
 template <int DT>
@@ -279,7 +288,7 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
         float top = s[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i]);
-        top = fmaxf(m, max_quarters(top));
+        top = fmaxf(m, max_quarters(top) - kLiftRows<DT>);
         const float base = top == -INFINITY ? 0.0f : top;
         const float alpha = __builtin_amdgcn_exp2f(m - base);
         m = top;
@@ -627,10 +636,12 @@ __global__ __launch_bounds__(W * 64, 2) void paged_tiles_kernel(const PagedParam
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
-        top = max_halves(top) * c;
-        // The maximum that the exponents are taken against follows only when it has fallen behind by 2^8: the sums are the same
-        // either way, and rescaling them in every step costs as much as a quarter of the exponentials.
-        if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) {
+        top = max_halves(top) * c - kLiftTiles<DT>;
+        // The base of the exponents follows the largest score only when that has passed it by kLag: rescaling the sums in every step
+        // costs as much as a quarter of the exponentials.  The largest probability is then rounded to 16 bits like the others (with a
+        // base that follows at once it is a power of two): over 8,192 random keys a bf16 result is off by 0.00234 of its norm instead of
+        // 0.00228, its own rounding among it.
+        if (__builtin_amdgcn_ballot_w64(top > m + kLag) != 0) {
             const float now = fmaxf(m, top);
             const float alpha = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.0f : now));
             m = now;

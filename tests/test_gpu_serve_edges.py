@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2504_18547_amd import vitq
-from tests.test_gpu_serve import BF16, F16, F32, _codes, _gen
+from tests import serve_reference as ref
+from tests.test_gpu_serve import BF16, F16, F32, F8, _codes, _gen, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +99,38 @@ def test_linear_sums_do_not_depend_on_where_results_go(M, K, N, out):
         y = torch.empty(M, (N + 15) // 16 * 16 + pad + 8, dtype=out, device="cuda")[:, first:first + N]
         vitq.vq_linear_e4m3(xm, wm, None, 0, y)
         assert torch.equal(y, ref_y), (pad, first)
+
+
+# ---- attention over the pages -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens", [1, 300])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype,cache", [(F16, F16), (F16, F8), (BF16, BF16)])
+@pytest.mark.parametrize("top", [0, 9000, 19999])
+def test_attention_many_small_probabilities(top, dtype, cache, D, tokens):
+    """One key far above 20,000 others, whose probabilities of e^-17.5 lie below half precision's smallest number but count together."""
+    n, page = 20000, 64
+    pages = -(-n // page)
+    g = _gen(top + D)
+    k = torch.zeros(pages * page, D)
+    k[top, 0], k[top, 1] = 16.0, 1.5
+    v = 300 + 50 * torch.rand(pages * page, D, generator=g)
+    v[top] = 1.0
+    kc, vc = [t.to(cache).view(pages, 1, page, D).cuda() for t in (k, v)]
+    obj = vitq.KvCache(kc, vc)
+    q = torch.zeros(tokens, D)
+    q[:, :2] = 1.0
+    table = torch.arange(pages, dtype=torch.int32).view(1, -1)
+    out, lse = torch.empty(tokens, D, dtype=dtype, device="cuda"), torch.empty(tokens, 1, device="cuda")
+    vitq.vq_attention_paged(q.to(dtype).cuda(), torch.tensor([0, tokens]).int().cuda(), torch.tensor([n]).int().cuda(), table.cuda(), obj,
+                            1.0, False, 0, 64, out, lse, None)        # (the hint keeps the keys in one piece)
+    o, l, mass, reach, total_v = ref.attention(q.double().view(tokens, 1, D), k.double()[:n].view(n, 1, D),
+                                               vc.cpu().double().view(-1, 1, D)[:n], torch.arange(n - tokens, n), 1.0, False, 0, n)
+    assert float((o - 1.0).abs().min()) > 0.1                         # the others matter
+    # A half-precision probability is kept times 2^7 at least, relative to the row's largest so far: what is lost of each is
+    # half of 2^-24 over 2^7 of that.  The rest as everywhere.
+    bound, lse_bound = ref.attention_bounds(o, l, mass, reach, torch.zeros_like(total_v), dtype, D, n)
+    if dtype == F16:
+        bound = bound + 2.0 ** -25 * 2.0 ** -7 * total_v
+    _within(out.view(tokens, 1, D), o, bound, "out")
+    _within(lse, l, lse_bound, "lse")
