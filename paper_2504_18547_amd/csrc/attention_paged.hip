@@ -214,6 +214,7 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
     for (int i = 0; i < NT; ++i) o[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
     const bool uneven = last_lo > lowest || first_hi < hi;        // the rows do not all see the same keys
+    auto partly = [&](int st) { const int key0 = lo + st * kStep; return key0 < last_lo || key0 + kStep > first_hi; };
     u32 odd = 0;
 
     // A step's operands as they lie in the cache.  They are requested a step before they are used, and their page numbers a step
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[4 * tt + i] = a[i] * p.scale_log2;
         }
-        if (x.seen != 0xFFFFFFFFu || key0 < last_lo || key0 + kStep > first_hi) {
+        if (x.seen != 0xFFFFFFFFu || partly(st)) {
             const u32 mine = x.seen >> (4 * q4);
             const int first = key0 + 4 * q4 - my_lo;              // this lane's key 0 against what its row sees
 #pragma unroll
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
                 // what is not in the cache must not reach the sums, not even times zero
                 if (!there) x.v[i] = 0;
             }
-            if (uneven) {
+            if (uneven && partly(st)) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -376,10 +377,13 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
     if (part_odd[0] | part_odd[1] | part_odd[2] | part_odd[3]) {
         int row_lo, row_hi;
         row_range(p, t, (int)divide(rr, p.group_div), row_lo, row_hi);
-        give_back(p, table, head_unit, lo + step0 * kStep, (step1 - step0) * kStep, row_lo, (u32)(row_hi - row_lo), [&](const uint8_t *v) {
+        for (int st = step0; st < step1; ++st) {
+            if (!partly(st)) continue;
+            give_back(p, table, head_unit, lo + st * kStep, kStep, row_lo, (u32)(row_hi - row_lo), [&](const uint8_t *v) {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) y[i] += odd_value<DT, C8>(v, c + i);
-        });
+                for (int i = 0; i < CH; ++i) y[i] += odd_value<DT, C8>(v, c + i);
+            });
+        }
     }
     const int token = t.first + (int)divide(rr, p.group_div);
     const int qh = head * p.group + rr - (int)divide(rr, p.group_div) * p.group;

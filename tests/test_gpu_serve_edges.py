@@ -6,7 +6,7 @@ import torch
 
 from paper_2504_18547_amd import vitq
 from tests import serve_reference as ref
-from tests.test_gpu_serve import BF16, F16, F32, F8, _codes, _gen, _within
+from tests.test_gpu_serve import BF16, F16, F32, F8, _check_attention, _codes, _gen, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -134,3 +134,17 @@ def test_attention_many_small_probabilities(top, dtype, cache, D, tokens):
         bound = bound + 2.0 ** -25 * 2.0 ** -7 * total_v
     _within(out.view(tokens, 1, D), o, bound, "out")
     _within(lse, l, lse_bound, "lse")
+
+
+@pytest.mark.parametrize("cache", [BF16, F8])
+@pytest.mark.parametrize("spots", [(2990,), (0, 2999), (37, 1500, 2998), (2999,)])
+def test_attention_values_that_are_not_finite_in_long_sequences(spots, cache):
+    """Few rows over many steps: infinities and NaN beside the mask's border, inside, and next to a page that is not there."""
+    def plant(obj, table):
+        page = obj.v.shape[2]
+        raw = obj.v.view(torch.uint8) if cache == F8 else obj.v
+        for i, key in enumerate(spots):
+            raw[int(table[0, key // page]), i % 2, key % page, 5 * i] = 0x7F if cache == F8 else float("inf" if i % 2 else "nan")
+    for causal, window in ((True, 0), (True, 40), (True, 2995), (False, 2980)):
+        _check_attention([(3, 3000), (11, 700)], 4, 2, 64, BF16, cache, page=16, causal=causal, window=window, edit=plant)
+    _check_attention([(3, 3000), (11, 700)], 4, 2, 128, BF16, cache, page=16, bad=((0, 1), (0, 100), (0, 184)), edit=plant)
