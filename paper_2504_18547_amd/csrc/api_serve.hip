@@ -214,8 +214,11 @@ vq_status vq_attention_paged(const void *q, int32_t dtype, int64_t tokens, int64
     const int64_t most = (int64_t)table_cols * cache->page_size;
     if (max_kv == 0 || max_kv > most) max_kv = most;
     if (window > (1 << 30)) window = 0;                       // reaches past every first key
-    // (a window shortens what a tile of rows sees; the workspace, which knows of none, is then more than enough)
-    const int64_t longest = window > 0 && window + 256 < max_kv ? window + 256 : max_kv;
+    // A window shortens what a tile of rows sees, to itself and the tile's tokens (up to 256) under the causal mask, and without it, when
+    // rows see up to the last key, to itself and the sequence's new tokens, of which the host knows the mean.  (The workspace, which
+    // knows of no window, is then more than enough.)
+    const int64_t mean = tokens / seqs, reach = window + (causal || mean < 256 ? 256 : mean);
+    const int64_t longest = window > 0 && reach < max_kv ? reach : max_kv;
     vitq::PagedParams p{};
     p.splits = vitq::paged_splits(tokens, seqs, q_heads, cache->heads, cache->head_dim, longest);
     const size_t need = split_bytes(p.splits, tokens, q_heads, cache->head_dim);

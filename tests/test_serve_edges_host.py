@@ -1,4 +1,5 @@
 """Host-side checks of the serving-layer operators: what the binding hands to the library (CPU only)."""
+import ctypes as C
 import os
 
 import pytest
@@ -27,3 +28,15 @@ def test_page_tables_whose_rows_overlap_are_refused(lib, monkeypatch):
         with pytest.raises(vitq.VitqError) as e:
             vitq.vq_attention_paged(q, offsets, lens, table, cache, 0.125, True, 0, 0, torch.empty_like(q), None, None)
         assert vitq.STATUS_NAMES[e.value.status] == "VQ_ERR_STRIDE"
+
+
+def test_windows_without_the_causal_mask_keep_their_splits(lib):
+    """Without the mask a row sees up to the last key, as far behind its window as there are new tokens: a chunk's keys are split over
+    workgroups (and need the workspace) as they are without the window; with the mask the window ends what a tile of rows sees."""
+    P = 0x10000                                 # an address that no call here may reach
+    c = vitq.vq_kv_cache(P, P, vitq.VQ_BF16, 1, 64, 16, 10000, 16 * 64, 16 * 64, 64, 1.0, 1.0)
+    n = C.c_size_t()
+    assert lib.vq_attention_paged_workspace(2000, 1, 1, C.byref(c), 2000, C.byref(n)) == 0 and n.value > 0
+    name = lambda causal, window: vitq.STATUS_NAMES[lib.vq_attention_paged(
+        P, vitq.VQ_BF16, 2000, 64, 1, P, P, 1, P, 4096, 4096, C.byref(c), 0.1, causal, window, 2000, P, 64, None, None, 0, None)]
+    assert name(1, 0) == name(0, 0) == name(0, 100) == "VQ_ERR_WORKSPACE"
