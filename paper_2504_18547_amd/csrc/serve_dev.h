@@ -67,10 +67,12 @@ __device__ __forceinline__ v4u widen8(u32 lo, u32 hi) {
     return r;
 }
 
-// 0.5 y (1 + tanh(..)) for any y: gelu_fast is for finite ones, and at +infinity takes infinity times zero from infinity.
+// 0.5 y (1 + tanh(sqrt(2 / pi) (y + 0.044715 y^3))) for any y, as y / (1 + 2^(w y)) with w = -2 log2(e) sqrt(2 / pi) (1 + 0.044715 y^2):
+// within 2^-21 of |y|; infinity at +infinity, where gelu_fast, which is for finite y, takes infinity times zero from it; NaN at
+// -infinity like the definition (times zero).
 __device__ __forceinline__ float gelu_any(float y) {
-    const float g = gelu_fast(y);
-    return y == INFINITY ? y : g;
+    const float w = fmaf(y * y, -0x1.a5a7d0p-4f, -0x1.26aec2p+1f);
+    return y * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(w * y));
 }
 
 // One element of any of the three input types.
