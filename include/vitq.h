@@ -477,7 +477,7 @@ typedef struct vq_rotate_desc {
  * are not wanted.  For E4M3 a value is multiplied by the fp32 reciprocal of the scale, limited to
  * +-448 and rounded (NaN stays NaN).  qkv and q_out: 16-byte aligned, with ld and q_ld multiples of 16
  * bytes; qkv must not overlap the outputs.  A token whose position lies outside the table is padding:
- * nothing of it is written.  A slot outside [0, pages*page_size) (-1, say) is not written.  The slots
+ * nothing of it is written (without rotation positions are not looked at).  A slot outside [0, pages*page_size) (-1, say) is not written.  The slots
  * that are written must differ from each other.  head_dim: a multiple of 8 up to 256 (E4M3: of 16);
  * tokens <= 2^23.
  * Errors: NULL, SHAPE, BITS (a dtype), STRIDE, STEP (eps, a scale), UNSUPPORTED.

@@ -413,7 +413,7 @@ __global__ __launch_bounds__(kWaves * 64, (DH == 64 ? 3 : 2) + (C8 ? 1 : 0)) voi
 // transposing LDS read, four keys of one channel per lane, in the order in which the score registers hold the keys; B = P^T.
 // LDS rows are unpadded with their 16-byte chunks permuted by the row: K's so that 16 rows' equal chunks cover all banks, V's so
 // that four rows' 64-byte pieces do.
-// 2 x 2,048 tokens over 8,192 keys, 32 / 8 heads of 128: 449-456 us, 1.06-1.07 PFLOP/s of the 1.43 that a large bf16 library product
+// 2 x 2,048 tokens over 8,192 keys, 32 / 8 heads of 128: 442-450 us, 1.07-1.09 PFLOP/s of the 1.43 that a large bf16 library product
 // reaches on this card (3 % of the time keeps infinities and NaN from rows that do not see their keys); the matrix cores are busy 57 % of the time, the rest goes to the issue of what stands between their
 // instructions (no loads: 391, no exponentials: 410).  Left out: steps of 32 keys (535), with them three waves a SIMD (535), the
 // exponentials of one step among the score products of the next in one wave (504, registers spill).
@@ -911,7 +911,11 @@ constexpr int kFewRows = 64, kWgRows = 256;
 
 // Which forms a batch needs; the host knows the totals alone.  A mean above kFewRows rows a sequence: tiles.  Below it the
 // streaming form, and both where one sequence can have a chunk of four tiles and more beside single tokens (each form then
-// passes over the other's sequences).
+// passes over the other's sequences).  us, streaming / tiles, 16 sequences over 4,096 keys: 16 / 4 heads of 128 with 48 rows each
+// 51.7 / 37.0, 64 51.5 / 37.6, 96 96.3 / 51.7, 128 116 / 53.5; 8 heads of 64 with 48 rows 46.0 / 64.5, 64 62.5 / 64.6, 96 86.2 / 67.0.
+// One chunk beside 63 single tokens over up to 8,000 keys, streaming alone / both: 16 heads of 64, 256 rows 211 / 324, 511 285 / 257,
+// 1,024 281 / 274, 2,048 331 / 306; 32 / 8 heads of 128, 280 rows 220 / 259, 512 293 / 264, 1,024 278 / 276, 2,044 491 / 291.  With a
+// window of 1,024 the second launch never pays: 511 rows of 64 53 / 93, 1,024 rows of 128 63 / 86, 2,044 85 / 88.
 struct Forms { bool few, many; };
 Forms forms_of(int64_t tokens, int seqs, int group) {
     if (tokens * group > (int64_t)kFewRows * seqs) return Forms{false, true};

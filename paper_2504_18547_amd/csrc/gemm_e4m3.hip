@@ -203,7 +203,7 @@ hipError_t launch_split(const GemmE4M3Params &p, hipStream_t stream) {
 // every row and the tokens' scales), S stages in LDS, filled by loads that go straight there.  LDS rows are unpadded, their
 // 16-byte chunks permuted by the row so that the sixteen rows of an operand spread over the banks; weight rows sit in an order
 // that gives a lane eight consecutive channels over two channel tiles.
-// 8192 x 4096 -> 8192: 254-260 us, 2.1 PFLOP/s; with one scale a tensor a library product reaches 3.2 on this card.  The matrix cores
+// 8192 x 4096 -> 8192: 258 us, with GELU 267 (three sets of buffers in turn), 2.1 PFLOP/s; with one scale a tensor a library product reaches 3.2 on this card.  The matrix cores
 // are busy 51 % of the time.  Without the FMAs that scale each block's products into the totals it took 27 us less, without the loads
 // to LDS 43, without the stores 34: they add up, for a SIMD's two waves issue little more than an instruction every four cycles.
 // Left out: products of the next stage's loads all at once (254 as well), 16 waves (registers spill).
@@ -458,11 +458,11 @@ hipError_t launch_tile(const GemmE4M3Params &p, hipStream_t stream) {
 //   (777 x 1000 -> 1000 7.6 / 10.9, K 1024 10.8 / 10.8, K 1536 15.5 / 13.8); 16 bits where K is ragged (7.2 / 8.0, K 896 9.7 / 7.6,
 //   K 1536 13.7 / 9.5) or the channels are, whose results leave as single stores (777 x 1000 -> 1001 7.5 / 10.2, 540 x 896 -> 1001
 //   8.2 / 9.5).  The rule looks at sizes alone, not at where the results go, so that equal products have equal bits.
-//   192 tiles of 256 x 256 and more fill the chip (8192 x 4096 -> 8192 254, with 128 x 128 tiles 337).  fp32 results, whose operands
-//   are widened in registers, do not gain from them (594 against 510).
+//   192 tiles of 256 x 256 and more fill the chip (8192 x 4096 -> 8192 258, with 128 x 128 tiles 345).  fp32 results, whose operands
+//   are widened in registers, do not gain from them (594 against 510, in one run).
 //   Up to 256 tiles of 64 x 128: a workgroup per CU, so four stages in its LDS and eight waves, two a SIMD, for one wave a SIMD issues
-//   an instruction every eight to ten cycles (512 x 4096 -> 4096 23.0, four waves 26.3, 128 x 128 on four waves 34).
-//   Else 128 x 128 on eight waves (1024 x 4096 -> 4096 30.2, on four 35.3), fp32 results past a round on four (510 / 541).
+//   an instruction every eight to ten cycles (512 x 4096 -> 4096 22.8, 128 x 128 on eight waves 28.0, 64 x 128 on four 26.3).
+//   Else 128 x 128 on eight waves (1024 x 4096 -> 4096 29.8, on four 35.3), fp32 results past a round on four (8192 x 4096 -> 8192 527 / 562).
 template <bool WIDE>
 hipError_t launch(const GemmE4M3Params &p, hipStream_t stream) {
     auto tiles = [&](int tokens, int channels) { return (int64_t)((p.M + tokens - 1) / tokens) * ((p.Nout + channels - 1) / channels); };
